@@ -168,7 +168,7 @@ def prepare(case, seed):
     if own:                                                   # the handle and the workspace that a program makes once and keeps
         from paper_2608_12932_b200 import binding as w4a8
         s["cache"] = w4a8.KV8Cache(s["k_codes"], s["v_codes"], s["k_scales"], s["v_scales"])
-        s["workspace"] = w4a8.new_kv8_workspace(n, t, c.get("q_heads", heads), s["cache"])
+        s["workspace"] = w4a8.new_kv8_workspace(s["cache"])
     return s
 
 
