@@ -46,7 +46,8 @@ typedef enum {
     W4A8_ERR_WORKSPACE = 4,  /* workspace_bytes < w4a8_workspace_bytes(M, N, K, group)       */
     W4A8_ERR_ARCH = 5,       /* current device is not sm_100                                 */
     W4A8_ERR_CUDA = 6,       /* a CUDA runtime/driver call failed                            */
-    W4A8_ERR_TIMEOUT = 7     /* a bounded device-side wait expired (seen via check_status)   */
+    W4A8_ERR_TIMEOUT = 7,    /* a bounded device-side wait expired (seen via check_status)   */
+    W4A8_ERR_INDEX = 8       /* a block number or position outside the cache (seen via check_status) */
 } w4a8_status;
 
 /* Which GEMM kernel family w4a8_gemm_path runs. */
@@ -255,6 +256,90 @@ w4a8_status w4a8_rope_shifted_keys(const void* k_pre_bf16, const int32_t* pos, i
 w4a8_status w4a8_streaming_mask(int views, int frames, int tokens_per_frame, uint8_t* mask, void* stream);
 
 /*
+ * Residual stream, root-mean-square norm and the quantisation of its result in one kernel: the step in front of the QKV
+ * and the gate+up projection (Sec. 3.5, "Kernel Fusion": element-wise steps are merged into their neighbours).
+ *   s[m,k] = bf16_rne(x[m,k] + r[m,k])                         or x itself without a residual
+ *   h[m,k] = bf16_rne(s[m,k] w[k] rstd[m]),  rstd[m] = 1 / sqrt(mean_k s[m,k]^2 + eps)      (fp32, one rounding)
+ *   (qa, sa, asum) = w4a8_quantize_act of h, bit-exact given h: the operands of w4a8_gemm
+ *   x         device, bf16 [M,K] row-major, 16-byte aligned, like residual, sum and h
+ *   residual  the same shape, or NULL
+ *   weight    device, bf16 [K], 16-byte aligned;  eps >= 0
+ *   sum       receives s; required with a residual and may be the same buffer as x or as the residual (a thread reads what
+ *             it then overwrites); NULL without a residual
+ *   h         receives h; may be NULL; not one of the other buffers
+ *   qa, sa, asum   as for w4a8_quantize_act
+ * Not-a-number and infinity in a row: that row's results are undefined, as for w4a8_quantize_act.
+ */
+w4a8_status w4a8_add_rmsnorm_quantize(const void* x_bf16, const void* residual_bf16, const void* weight_bf16, float eps,
+                                      int M, int K, int group, void* sum_bf16, void* h_bf16,
+                                      int8_t* qa, uint16_t* sa, int32_t* asum, void* stream);
+
+/*
+ * A cache of keys and values held in 8 bits with one fp16 scale for each block of tokens and head, and the attention that reads it:
+ * what stands between the QKV and the O projection of a decoder layer (the paper's streaming inference keeps the keys and
+ * values of a window of frames, Sec. 3.1; it names no format for them, this is the one of the activations, per block).
+ *
+ *   k_codes, v_codes    int8 [num_blocks][heads][block][dim], 16-byte aligned; a key or value is its code times the scale of
+ *   k_scales, v_scales  fp16 [num_blocks][heads], not negative          its block and head
+ *   block 16, 32, 64 or 128 tokens;  dim 64 or 128;  heads = key/value heads
+ * A sequence is a list of blocks: table int32 [B][table_width], entry i the number of the block that holds positions
+ * i block .. i block + block - 1.  Several sequences may read one block.  Entries past a sequence's last position are not read.
+ * All of it is device memory of the caller's.  The struct itself is host memory, read during the call.
+ *
+ * A block number outside 0 .. num_blocks - 1 where one is needed is never followed: its positions are left out (nothing is
+ * stored, nothing is read), and the workspace's status word becomes W4A8_ERR_INDEX (w4a8_check_status).  So it is for a
+ * negative start, and for positions beyond table_width blocks.
+ */
+typedef struct {
+    int8_t *k_codes, *v_codes;
+    uint16_t *k_scales, *v_scales;
+    int num_blocks, heads, dim, block;
+} w4a8_kv8_cache;
+
+/*
+ * Appends T tokens' keys and values to each of B sequences: token i of sequence b goes to position start[b] + i, for i <
+ * count[b].  For each block and head touched, K and V apart, with old the tokens in front of the new ones in that block:
+ *   s  = max(s_old, fp16_rne(min(max |new| / 127, 65504)))       s_old = 0 where there are no old ones
+ *   old codes     q' = rne(q s_old / s)         (unchanged where the scale is)
+ *   new codes     q = clamp(rne(x / s), -127, 127);              all codes 0 where s = 0
+ * Both quotients are those of exact arithmetic, ties to even.  So a block's scale never falls while tokens are added to it, and starts
+ * anew when its first token is written.  Slots behind the new tokens keep what they hold; writing again from an earlier
+ * position (draft tokens that were not accepted) is an append like any other.
+ *   k, v      device, bf16, 16-byte aligned: row b T + i holds heads x dim contiguous values, rows k_stride and v_stride
+ *             elements apart (multiples of 8, at least heads dim): columns of a QKV projection's output serve as they are
+ *   start     device, int32 [B];  count  device, int32 [B] (values outside 0 .. T count as the nearest), or NULL: T each
+ *   workspace at least W4A8_WORKSPACE_HEADER_BYTES, initialised (w4a8_workspace_init): its status word
+ * The blocks that one call writes must be distinct, and not written by another call at the same time.
+ * Run again on the same input it changes nothing.  B, 2 heads <= 65535.
+ */
+w4a8_status w4a8_kv8_append(const w4a8_kv8_cache* cache, const void* k_bf16, const void* v_bf16, long long k_stride,
+                            long long v_stride, int B, int T, const int32_t* table, int table_width, const int32_t* start,
+                            const int32_t* count, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention of T new tokens of each of B sequences over the cache, q_heads query heads in groups of q_heads / heads per key
+ * head (query head h reads key head h / (q_heads / heads)):
+ *   out[b,t,h,:] = sum_{j < limits[b,t]} p_j v_j / sum p_j,   p_j = exp(scale q[b,t,h,:] . k_j)
+ * limits[b][t] is the number of leading positions that token t sees: its own position + 1 for causal attention (after the
+ * append), the row sums of w4a8_streaming_mask for streaming prefill, the sequence's length where all is seen, 0 for a row of a
+ * padded batch (its output is 0).  Values outside 0 .. table_width block count as the nearest.
+ * Codes are multiplied as fp16, exactly; q is too (elements below 2^-31 of their row's largest are cut short); weights are
+ * rounded to fp16 for the second product, sums and softmax statistics are fp32; one rounding to bf16.  Judged against the
+ * fp64 definition.  A row of q with an infinity or not-a-number gives not-a-number in that row alone.
+ *   q         device, bf16, 16-byte aligned: row b T + t holds q_heads x dim contiguous values, rows q_stride elements apart
+ *             (a multiple of 8, at least q_heads dim)
+ *   limits    device, int32 [B][T];  out  device, bf16 [B T][q_heads dim], 16-byte aligned
+ *   workspace at least w4a8_kv8_workspace_bytes(dim) bytes, 256-byte aligned, initialised once; the same rules as for
+ *             w4a8_gemm, with whose calls it may be shared on one stream.  Enough for any call of this dim; 0: unsupported dim
+ * Results are run-to-run deterministic.  W4A8_ERR_SHAPE also for q_heads not a multiple of heads, more than 65535 / heads
+ * sequences, 2^31 or more rows T q_heads / heads, or B x T >= 2^31.
+ */
+size_t w4a8_kv8_workspace_bytes(int dim);
+w4a8_status w4a8_kv8_attention(const w4a8_kv8_cache* cache, const void* q_bf16, long long q_stride, int B, int T, int q_heads,
+                               const int32_t* table, int table_width, const int32_t* limits, float scale, void* out_bf16,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * The weight-only variant the paper contrasts W4A8 with (Sec. 3.4, first paragraph: 4-bit weights with 16-bit
  * activations shrink what the memory-bound decode must load, and leave the arithmetic of the compute-bound
  * prefill in 16-bit floating point).  Same packed weights, activations NOT quantised:
@@ -374,9 +459,9 @@ w4a8_status w4a8_selftest_wait_timeout(const int8_t* qa, const uint16_t* sa, con
                                        size_t workspace_bytes, void* stream);
 
 /*
- * Reads back the workspace status word: synchronises `stream`, returns W4A8_OK or
- * W4A8_ERR_TIMEOUT (a kernel gave up on a bounded wait; its output is then invalid), and
- * clears the word.  Host-synchronising: for tests and debugging, not for the hot path.
+ * Reads back the workspace status word: synchronises `stream`, returns W4A8_OK,
+ * W4A8_ERR_TIMEOUT (a kernel gave up on a bounded wait; its output is then invalid) or W4A8_ERR_INDEX
+ * (a kernel of the 8-bit cache met a block number or position that does not exist), and clears the word.  Host-synchronising: for tests and debugging, not for the hot path.
  */
 w4a8_status w4a8_check_status(void* workspace, void* stream);
 

@@ -13,7 +13,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libw4a8.so")
 
 GROUP = 128
-OK, ERR_NULL, ERR_SHAPE, ERR_ALIGN, ERR_WORKSPACE, ERR_ARCH, ERR_CUDA, ERR_TIMEOUT = range(8)
+OK, ERR_NULL, ERR_SHAPE, ERR_ALIGN, ERR_WORKSPACE, ERR_ARCH, ERR_CUDA, ERR_TIMEOUT, ERR_INDEX = range(9)
 PATH_AUTO, PATH_SPLITK, PATH_TCGEN05, PATH_SPLITK_WORKSPACE, PATH_STRIP = 0, 1, 2, 3, 4
 WORKSPACE_HEADER_BYTES = 4096
 WORKSPACE_ZEROED_BYTES = 4096 + 192 * 16384
@@ -24,7 +24,8 @@ EXPORTS = ("w4a8_status_string", "w4a8_packed_bytes", "w4a8_workspace_bytes", "w
            "w4a8_gemm_per_channel", "w4a8_static_scratch_status", "w4a8_selftest_wait_timeout",
            "w4a8_silu_mul_quantize", "w4a8_gate_up_form", "w4a8_gate_up_silu_quantize", "w4a8_a16_gemm",
            "w4a8_dequantize_weights", "w4a8_gemm_residual", "w4a8_rope_shifted_keys",
-           "w4a8_streaming_mask")
+           "w4a8_streaming_mask", "w4a8_add_rmsnorm_quantize", "w4a8_kv8_append", "w4a8_kv8_workspace_bytes",
+           "w4a8_kv8_attention")
 
 _lib = None
 
@@ -72,6 +73,15 @@ def lib():
         L.w4a8_rope_shifted_keys.argtypes = [vp, vp, ci, ci, ci, ci, ctypes.c_double, vp, vp]
         L.w4a8_streaming_mask.restype = ci
         L.w4a8_streaming_mask.argtypes = [ci, ci, ci, vp, vp]
+        cf, ll = ctypes.c_float, ctypes.c_longlong
+        L.w4a8_add_rmsnorm_quantize.restype = ci
+        L.w4a8_add_rmsnorm_quantize.argtypes = [vp, vp, vp, cf, ci, ci, ci, vp, vp, vp, vp, vp, vp]
+        L.w4a8_kv8_append.restype = ci
+        L.w4a8_kv8_append.argtypes = [vp, vp, vp, ll, ll, ci, ci, vp, ci, vp, vp, vp, sz, vp]
+        L.w4a8_kv8_workspace_bytes.restype = sz
+        L.w4a8_kv8_workspace_bytes.argtypes = [ci]
+        L.w4a8_kv8_attention.restype = ci
+        L.w4a8_kv8_attention.argtypes = [vp, vp, ll, ci, ci, ci, vp, ci, vp, cf, vp, vp, sz, vp]
         L.w4a8_gemm_residual.restype = ci
         L.w4a8_gemm_residual.argtypes = [ci, vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, vp, sz, vp]
         L.w4a8_a16_gemm.restype = ci
@@ -307,6 +317,150 @@ def w4a8_streaming_mask(views, frames, tokens_per_frame, device="cuda", stream=N
     mask = torch.empty((views * tokens_per_frame, views * frames * tokens_per_frame), dtype=torch.uint8, device=device)
     _check(lib().w4a8_streaming_mask(views, frames, tokens_per_frame, _ptr(mask), _stream(stream)), "w4a8_streaming_mask")
     return mask
+
+
+def _here(*tensors):
+    """The tensors (None among them allowed) must lie on the current device, where the call enqueues its work."""
+    index = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            raise TypeError(f"need tensors on the current device, cuda:{index}, got {t.device}")
+
+
+def w4a8_add_rmsnorm_quantize(x, weight, eps, residual=None, group=GROUP, sum_out=None, h_out=None, out=None, stream=None):
+    """x, residual bf16 [M,K], weight bf16 [K] -> (s, qa int8 [M,K], sa fp16 [M], asum int32 [M,K/group]): s = x + residual in
+    bf16 (x itself without a residual), the rest w4a8_quantize_act of its root-mean-square norm times weight.
+    sum_out may be x or residual; h_out receives the normed row in bf16; out = (qa, sa, asum)."""
+    _dev(x, torch.bfloat16, "x"), _dev(weight, torch.bfloat16, "weight")
+    M, K = x.shape
+    if weight.shape != (K,) or (residual is not None and residual.shape != x.shape):
+        raise W4A8Error(ERR_SHAPE, "w4a8_add_rmsnorm_quantize")
+    total = x
+    if residual is not None:
+        _dev(residual, torch.bfloat16, "residual")
+        total = torch.empty_like(x) if sum_out is None else _dev(sum_out, torch.bfloat16, "sum_out")
+    if out is None:
+        out = (torch.empty((M, K), dtype=torch.int8, device=x.device), torch.empty((M,), dtype=torch.float16, device=x.device),
+               torch.empty((M, max(K // group, 0)), dtype=torch.int32, device=x.device))
+    qa, sa, asum = out
+    _dev(qa, torch.int8, "qa"), _dev(sa, torch.float16, "sa"), _dev(asum, torch.int32, "asum")
+    if h_out is not None:
+        _dev(h_out, torch.bfloat16, "h_out")
+    if (total.shape != x.shape or qa.shape != x.shape or sa.shape != (M,) or asum.numel() != M * (K // group) or
+            (h_out is not None and h_out.shape != x.shape)):
+        raise W4A8Error(ERR_SHAPE, "w4a8_add_rmsnorm_quantize")
+    _here(x, weight, residual, total, h_out, qa, sa, asum)
+    _check(lib().w4a8_add_rmsnorm_quantize(x.data_ptr(), _ptr(residual), weight.data_ptr(), eps, M, K, group,
+                                           total.data_ptr() if residual is not None else None, _ptr(h_out), qa.data_ptr(),
+                                           sa.data_ptr(), asum.data_ptr(), _stream(stream)), "w4a8_add_rmsnorm_quantize")
+    return total, qa, sa, asum
+
+
+class _KV8Struct(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("num_blocks", ctypes.c_int), ("heads", ctypes.c_int), ("dim", ctypes.c_int), ("block", ctypes.c_int)]
+
+
+class KV8Cache:
+    """An 8-bit key/value cache (w4a8_kv8_cache in the header) over tensors of the caller's: codes int8 [num_blocks, heads, block,
+    dim], scales fp16 [num_blocks, heads].  KV8Cache.empty allocates them."""
+
+    def __init__(self, k_codes, v_codes, k_scales, v_scales):
+        for t, dtype, name in ((k_codes, torch.int8, "k_codes"), (v_codes, torch.int8, "v_codes"),
+                               (k_scales, torch.float16, "k_scales"), (v_scales, torch.float16, "v_scales")):
+            _dev(t, dtype, name)
+            if t.get_device() != k_codes.get_device():
+                raise TypeError(f"{name}: on {t.device}, k_codes on {k_codes.device}")
+        if k_codes.dim() != 4 or v_codes.shape != k_codes.shape or k_scales.shape != k_codes.shape[:2] or v_scales.shape != k_codes.shape[:2]:
+            raise W4A8Error(ERR_SHAPE, "KV8Cache")
+        self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales
+        self.num_blocks, self.heads, self.block, self.dim = k_codes.shape
+        self._struct = _KV8Struct(k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
+                                  self.num_blocks, self.heads, self.dim, self.block)
+        self._address = ctypes.addressof(self._struct)
+
+    @classmethod
+    def empty(cls, num_blocks, heads, dim, block=64, device="cuda"):
+        codes = [torch.empty((num_blocks, heads, block, dim), dtype=torch.int8, device=device) for _ in range(2)]
+        scales = [torch.empty((num_blocks, heads), dtype=torch.float16, device=device) for _ in range(2)]
+        return cls(*codes, *scales)
+
+
+def w4a8_kv8_workspace_bytes(dim):
+    return int(lib().w4a8_kv8_workspace_bytes(dim))
+
+
+def new_kv8_workspace(cache, stream=None):
+    """Allocates (through torch) and initialises a workspace for w4a8_kv8_append and w4a8_kv8_attention on this cache."""
+    nbytes = w4a8_kv8_workspace_bytes(cache.dim)
+    if nbytes == 0:
+        raise W4A8Error(ERR_SHAPE, "w4a8_kv8_workspace_bytes")
+    _here(cache.k_codes)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.k_codes.device)
+    _check(lib().w4a8_workspace_init(_ptr(ws), nbytes, _stream(stream)), "w4a8_workspace_init")
+    return ws
+
+
+def _heads_view(t, heads, dim, name):
+    """The row stride of a bf16 CUDA tensor [tokens, heads, dim] whose rows are contiguous (a column range of a wider matrix, say)."""
+    if not (t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 3):
+        raise TypeError(f"{name}: need a CUDA tensor [tokens, heads, dim] of bf16, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    tokens, h, d = t.shape
+    if d != dim or (heads is not None and h != heads):
+        raise W4A8Error(ERR_SHAPE, name)
+    s0, s1, s2 = t.stride()
+    if s2 != 1 or (s1 != dim and h > 1):
+        raise TypeError(f"{name}: a token's heads x dim values must be contiguous, got strides {t.stride()}")
+    return s0 if tokens > 1 else h * dim
+
+
+def w4a8_kv8_append(cache, k, v, table, start, workspace, count=None, stream=None):
+    """Appends k, v bf16 [B*T, heads, dim] (rows may be columns of a wider matrix) to the sequences whose blocks are table int32
+    [B, width]: token i of sequence b to position start[b] + i, for i < count[b] (all T without count)."""
+    k_stride, v_stride = _heads_view(k, cache.heads, cache.dim, "k"), _heads_view(v, cache.heads, cache.dim, "v")
+    _dev(start, torch.int32, "start"), _dev(workspace, torch.uint8, "workspace")
+    _dev(table, torch.int32, "table")
+    tokens = k.shape[0]
+    if table.dim() != 2 or (tokens % table.shape[0] if table.shape[0] else tokens):
+        raise W4A8Error(ERR_SHAPE, "w4a8_kv8_append")
+    B = table.shape[0]
+    T = tokens // B if B else 0
+    if v.shape != k.shape or start.shape != (B,) or (count is not None and _dev(count, torch.int32, "count").shape != (B,)):
+        raise W4A8Error(ERR_SHAPE, "w4a8_kv8_append")
+    _here(k, v, table, start, count, workspace, cache.k_codes)
+    _check(lib().w4a8_kv8_append(cache._address, k.data_ptr(), v.data_ptr(), k_stride, v_stride, B, T, table.data_ptr(), table.shape[1],
+                                 start.data_ptr(), _ptr(count), workspace.data_ptr(), workspace.numel(), _stream(stream)),
+           "w4a8_kv8_append")
+
+
+def w4a8_kv8_attention(q, cache, table, limits, scale, workspace, out=None, stream=None):
+    """out bf16 [B*T, q_heads*dim]: q bf16 [B*T, q_heads, dim] (rows may be columns of a wider matrix) over the cache; token t of
+    sequence b sees positions 0 .. limits[b, t] - 1 of the blocks in table int32 [B, width]."""
+    q_stride = _heads_view(q, None, cache.dim, "q")
+    _dev(limits, torch.int32, "limits"), _dev(workspace, torch.uint8, "workspace")
+    _dev(table, torch.int32, "table")
+    tokens, q_heads, dim = q.shape
+    if limits.dim() != 2 or table.dim() != 2 or table.shape[0] != limits.shape[0] or limits.numel() != tokens:
+        raise W4A8Error(ERR_SHAPE, "w4a8_kv8_attention")
+    B, T = limits.shape
+    if out is None:
+        out = torch.empty((tokens, q_heads * dim), dtype=torch.bfloat16, device=q.device)
+    else:
+        _dev(out, torch.bfloat16, "out")
+    if out.numel() != tokens * q_heads * dim:
+        raise W4A8Error(ERR_SHAPE, "w4a8_kv8_attention")
+    _here(q, table, limits, workspace, out, cache.k_codes)
+    _check(lib().w4a8_kv8_attention(cache._address, q.data_ptr(), q_stride, B, T, q_heads, table.data_ptr(), table.shape[1],
+                                    limits.data_ptr(), scale, out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream(stream)),
+           "w4a8_kv8_attention")
+    return out
+
+
+def streaming_limits(views, frames, tokens_per_frame):
+    """Row sums of the streaming mask: how many leading positions each of the newest frames' tokens sees, int32 [views * n] (CPU).
+    Index arithmetic only."""
+    v, i = torch.arange(views, dtype=torch.int32)[:, None], torch.arange(tokens_per_frame, dtype=torch.int32)[None, :]
+    return ((v * frames + frames - 1) * tokens_per_frame + i + 1).reshape(-1)
 
 
 def w4a8_a16_gemm(x, packed_w, N, workspace, group=GROUP, out=None, stream=None):

@@ -113,6 +113,7 @@ const char* w4a8_status_string(w4a8_status s) {
         case W4A8_ERR_ARCH: return "device is not sm_100";
         case W4A8_ERR_CUDA: return "CUDA call failed";
         case W4A8_ERR_TIMEOUT: return "device-side wait timed out";
+        case W4A8_ERR_INDEX: return "block number or position outside the cache";
     }
     return "unknown status";
 }
@@ -304,6 +305,80 @@ w4a8_status w4a8_rope_shifted_keys(const void* k_pre_bf16, const int32_t* pos, i
                ? W4A8_OK : W4A8_ERR_CUDA;
 }
 
+w4a8_status w4a8_add_rmsnorm_quantize(const void* x_bf16, const void* residual_bf16, const void* weight_bf16, float eps, int M, int K,
+                                      int group, void* sum_bf16, void* h_bf16, int8_t* qa, uint16_t* sa, int32_t* asum, void* stream) {
+    if (group != GROUP || K <= 0 || K % GROUP != 0 || M < 0 || !(eps >= 0.0f)) return W4A8_ERR_SHAPE;
+    if (M == 0) return W4A8_OK;
+    if (!x_bf16 || !weight_bf16 || !qa || !sa || !asum || (residual_bf16 && !sum_bf16)) return W4A8_ERR_NULL;
+    if (!aligned(x_bf16, 16) || !aligned(residual_bf16, 16) || !aligned(weight_bf16, 16) || !aligned(sum_bf16, 16) || !aligned(h_bf16, 16) ||
+        !aligned(qa, 16) || !aligned(sa, 2) || !aligned(asum, 4))
+        return W4A8_ERR_ALIGN;
+    w4a8_status a = arch_check();
+    if (a != W4A8_OK) return a;
+    return launch_add_rmsnorm_quantize(x_bf16, residual_bf16, weight_bf16, eps, M, K, sum_bf16, h_bf16, qa, sa, asum,
+                                       static_cast<cudaStream_t>(stream)) == cudaSuccess ? W4A8_OK : W4A8_ERR_CUDA;
+}
+
+// what both calls on a cache ask of it and of the sequences
+static w4a8_status check_kv8(const w4a8_kv8_cache* c, int B, int T, int table_width) {
+    if (!c) return W4A8_ERR_NULL;
+    if (c->num_blocks <= 0 || c->heads <= 0 || (c->dim != 64 && c->dim != 128) ||
+        (c->block != 16 && c->block != 32 && c->block != 64 && c->block != 128) || B < 0 || T < 0 || table_width <= 0)
+        return W4A8_ERR_SHAPE;
+    if (c->heads > 32767 || (long long)B * c->heads > 65535 || (long long)B * T > 0x7FFFFFFFll) return W4A8_ERR_SHAPE;
+    return W4A8_OK;
+}
+static w4a8_status check_kv8_pointers(const w4a8_kv8_cache* c) {
+    if (!c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales) return W4A8_ERR_NULL;
+    if (!aligned(c->k_codes, 16) || !aligned(c->v_codes, 16) || !aligned(c->k_scales, 2) || !aligned(c->v_scales, 2)) return W4A8_ERR_ALIGN;
+    return W4A8_OK;
+}
+
+w4a8_status w4a8_kv8_append(const w4a8_kv8_cache* cache, const void* k_bf16, const void* v_bf16, long long k_stride, long long v_stride,
+                            int B, int T, const int32_t* table, int table_width, const int32_t* start, const int32_t* count,
+                            void* workspace, size_t workspace_bytes, void* stream) {
+    w4a8_status s = check_kv8(cache, B, T, table_width);
+    if (s != W4A8_OK) return s;
+    const long long row = (long long)cache->heads * cache->dim;
+    if (k_stride % 8 != 0 || v_stride % 8 != 0 || k_stride < row || v_stride < row) return W4A8_ERR_SHAPE;
+    if (B == 0 || T == 0) return W4A8_OK;
+    if (!k_bf16 || !v_bf16 || !table || !start || !workspace) return W4A8_ERR_NULL;
+    s = check_kv8_pointers(cache);
+    if (s != W4A8_OK) return s;
+    if (!aligned(k_bf16, 16) || !aligned(v_bf16, 16) || !aligned(table, 4) || !aligned(start, 4) || !aligned(count, 4) || !aligned(workspace, 256))
+        return W4A8_ERR_ALIGN;
+    if (workspace_bytes < WS_HEADER_BYTES) return W4A8_ERR_WORKSPACE;
+    w4a8_status a = arch_check();
+    if (a != W4A8_OK) return a;
+    return launch_kv8_append(*cache, k_bf16, v_bf16, k_stride, v_stride, B, T, table, table_width, start, count,
+                             reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(workspace) + WS_STATUS_OFF),
+                             static_cast<cudaStream_t>(stream)) == cudaSuccess ? W4A8_OK : W4A8_ERR_CUDA;
+}
+
+size_t w4a8_kv8_workspace_bytes(int dim) {
+    return dim == 64 || dim == 128 ? WS_SHARED_OFF + kv8_partial_bytes(dim, device_sm_count()) : 0;
+}
+
+w4a8_status w4a8_kv8_attention(const w4a8_kv8_cache* cache, const void* q_bf16, long long q_stride, int B, int T, int q_heads,
+                               const int32_t* table, int table_width, const int32_t* limits, float scale, void* out_bf16,
+                               void* workspace, size_t workspace_bytes, void* stream) {
+    w4a8_status s = check_kv8(cache, B, T, table_width);
+    if (s != W4A8_OK) return s;
+    if (q_heads <= 0 || q_heads % cache->heads != 0 || q_stride % 8 != 0 || q_stride < (long long)q_heads * cache->dim ||
+        (long long)T * (q_heads / cache->heads) > 0x7FFFFFFFll)
+        return W4A8_ERR_SHAPE;
+    if (B == 0 || T == 0) return W4A8_OK;
+    if (!q_bf16 || !table || !limits || !out_bf16 || !workspace) return W4A8_ERR_NULL;
+    s = check_kv8_pointers(cache);
+    if (s != W4A8_OK) return s;
+    if (!aligned(q_bf16, 16) || !aligned(table, 4) || !aligned(limits, 4) || !aligned(out_bf16, 16) || !aligned(workspace, 256)) return W4A8_ERR_ALIGN;
+    if (workspace_bytes < w4a8_kv8_workspace_bytes(cache->dim)) return W4A8_ERR_WORKSPACE;
+    w4a8_status a = arch_check();
+    if (a != W4A8_OK) return a;
+    return launch_kv8_attention(*cache, q_bf16, q_stride, B, T, q_heads, table, table_width, limits, scale, out_bf16, workspace,
+                                static_cast<cudaStream_t>(stream)) == cudaSuccess ? W4A8_OK : W4A8_ERR_CUDA;
+}
+
 w4a8_status w4a8_streaming_mask(int views, int frames, int tokens_per_frame, uint8_t* mask, void* stream) {
     if (views <= 0 || frames <= 0 || tokens_per_frame <= 0) return W4A8_ERR_SHAPE;
     if (!mask) return W4A8_ERR_NULL;
@@ -455,7 +530,7 @@ w4a8_status w4a8_check_status(void* workspace, void* stream) {
     if (word == 0) return W4A8_OK;
     if (cudaMemsetAsync(static_cast<uint8_t*>(workspace) + WS_STATUS_OFF, 0, 4, st) != cudaSuccess) return W4A8_ERR_CUDA;
     if (cudaStreamSynchronize(st) != cudaSuccess) return W4A8_ERR_CUDA;
-    return word == W4A8_ERR_TIMEOUT ? W4A8_ERR_TIMEOUT : W4A8_ERR_CUDA;
+    return word == W4A8_ERR_TIMEOUT || word == W4A8_ERR_INDEX ? (w4a8_status)word : W4A8_ERR_CUDA;
 }
 
 w4a8_status w4a8_selftest_wait_timeout(const int8_t* qa, const uint16_t* sa, const int32_t* asum, const void* packed_w,

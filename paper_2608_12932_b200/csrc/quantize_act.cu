@@ -22,43 +22,6 @@ namespace {
 
 constexpr int QA_CACHE_CHUNKS = 1536;   // 16-byte chunks of a row kept in registers: rows up to 12288 read once
 
-__device__ __forceinline__ uint32_t absmax_bits_bf16x8(const uint4& v, uint32_t run) {
-    // bf16 magnitudes order like their 15-bit patterns: keep a packed running max of two lanes
-    run = __vmaxu2(run, v.x & 0x7FFF7FFFu);
-    run = __vmaxu2(run, v.y & 0x7FFF7FFFu);
-    run = __vmaxu2(run, v.z & 0x7FFF7FFFu);
-    run = __vmaxu2(run, v.w & 0x7FFF7FFFu);
-    return run;
-}
-
-__device__ __forceinline__ uint2 quant8(const uint4& v, float s, int& sum) {
-    int q0 = quant1(v.x << 16, s), q1 = quant1(v.x & 0xFFFF0000u, s);
-    int q2 = quant1(v.y << 16, s), q3 = quant1(v.y & 0xFFFF0000u, s);
-    int q4 = quant1(v.z << 16, s), q5 = quant1(v.z & 0xFFFF0000u, s);
-    int q6 = quant1(v.w << 16, s), q7 = quant1(v.w & 0xFFFF0000u, s);
-    sum = q0 + q1 + q2 + q3 + q4 + q5 + q6 + q7;
-    uint2 o;
-    o.x = (q0 & 0xFF) | ((q1 & 0xFF) << 8) | ((q2 & 0xFF) << 16) | ((uint32_t)q3 << 24);
-    o.y = (q4 & 0xFF) | ((q5 & 0xFF) << 8) | ((q6 & 0xFF) << 16) | ((uint32_t)q7 << 24);
-    return o;
-}
-
-// Fast path of a chunk (see the header): products with the row's reciprocal scale.  `worst` returns the largest
-// distance of a product from the integer it was rounded to.  Valid for rows whose scale did not saturate
-// (|x / s_a| < 127.1, so the rounded value needs no clamp).
-__device__ __forceinline__ uint32_t quant4_fast(uint32_t lo_pair, uint32_t hi_pair, float rinv, float& worst) {
-    constexpr float MAGIC = 12582912.0f;                     // 1.5 * 2^23: adding it rounds to an integer, ties to even
-    const float t0 = __fmul_rn(__uint_as_float(lo_pair << 16), rinv), t1 = __fmul_rn(__uint_as_float(lo_pair & 0xFFFF0000u), rinv);
-    const float t2 = __fmul_rn(__uint_as_float(hi_pair << 16), rinv), t3 = __fmul_rn(__uint_as_float(hi_pair & 0xFFFF0000u), rinv);
-    const float y0 = __fadd_rn(t0, MAGIC), y1 = __fadd_rn(t1, MAGIC), y2 = __fadd_rn(t2, MAGIC), y3 = __fadd_rn(t3, MAGIC);
-    worst = fmaxf(worst, fmaxf(fmaxf(fabsf(__fsub_rn(t0, __fsub_rn(y0, MAGIC))), fabsf(__fsub_rn(t1, __fsub_rn(y1, MAGIC)))),
-                               fmaxf(fabsf(__fsub_rn(t2, __fsub_rn(y2, MAGIC))), fabsf(__fsub_rn(t3, __fsub_rn(y3, MAGIC))))));
-    // low mantissa bytes of y0..y3 -> one word
-    const uint32_t a = __byte_perm(__float_as_uint(y0), __float_as_uint(y1), 0x0040);
-    const uint32_t b = __byte_perm(__float_as_uint(y2), __float_as_uint(y3), 0x0040);
-    return __byte_perm(a, b, 0x5410);
-}
-
 // QA_THREADS threads per token row: 256 for many rows (more rows in flight per SM), 512 or 1024 for fewer
 // (a row's latency chain - load, row maximum, divisions, store - is then shorter per thread).
 // QA_CACHE: 16-byte chunks per thread kept in registers between the two passes (rows up to QA_THREADS * QA_CACHE * 8

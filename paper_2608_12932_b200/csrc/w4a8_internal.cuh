@@ -112,6 +112,17 @@ cudaError_t launch_gemm_strip(const int8_t* qa, const uint16_t* sa, const int32_
 cudaError_t launch_rope_shifted_keys(const void* k_pre, const int32_t* pos, int delta, int T, int H, int D, double base,
                                      void* k_rot, cudaStream_t stream);
 cudaError_t launch_streaming_mask(int V, int F, int n, uint8_t* mask, cudaStream_t stream);
+// residual add, root-mean-square norm and activation quantisation of M rows; residual and h_out may be null
+cudaError_t launch_add_rmsnorm_quantize(const void* x, const void* residual, const void* weight, float eps, int M, int K, void* sum_out,
+                                        void* h_out, int8_t* qa, uint16_t* sa, int32_t* asum, cudaStream_t stream);
+// 8-bit key/value cache (w4a8_kv8_cache in the public header): append, attention.  Strides in elements; arguments checked by the caller.
+inline int kv8_log2(int block) { return block == 16 ? 4 : (block == 32 ? 5 : (block == 64 ? 6 : 7)); }
+cudaError_t launch_kv8_append(const w4a8_kv8_cache& c, const void* k, const void* v, long long k_stride, long long v_stride, int B, int T,
+                              const int32_t* table, int table_width, const int32_t* start, const int32_t* count, uint32_t* status,
+                              cudaStream_t stream);
+size_t kv8_partial_bytes(int dim, int sms);   // the attention kernels' sums of key slices, in the workspace from WS_SHARED_OFF on
+cudaError_t launch_kv8_attention(const w4a8_kv8_cache& c, const void* q, long long q_stride, int B, int T, int q_heads, const int32_t* table,
+                                 int table_width, const int32_t* limits, float scale, void* out, void* workspace, cudaStream_t stream);
 // W4A16 (bf16 activations against the same packed weights), up to STRIP_MAX_M tokens
 bool a16_supported(int M, int N, int K);
 void a16_plan(int M, int N, int K, int* strip_rows, int* ctas);
