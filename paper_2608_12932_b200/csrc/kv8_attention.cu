@@ -446,29 +446,29 @@ cudaError_t launch_combine(const AttendArgs& a, int B, int tile_rows, cudaStream
 
 }  // namespace
 
-// Row tiles of 16 with three CTAs per SM, of 32 with two: what is resident at once.
-static int rows_ctas_per_sm(int rows) { return rows == 16 ? 3 : 2; }
+// Row tiles of 16 with three CTAs per SM, of 32 with two, of 256 with one: what is resident at once.
+static int ctas_per_sm(int rows) { return rows == 16 ? 3 : (rows == 32 ? 2 : 1); }
 
-Kv8Plan kv8_plan(int B, int T, int q_heads, int kv_heads, int /*dim*/, long long max_keys, int sms) {
+Kv8Plan kv8_plan(int B, int T, int q_heads, int kv_heads, long long max_keys, int sms) {
     Kv8Plan p;
     const long long rows = (long long)T * (q_heads / kv_heads);
-    p.rows = rows <= 16 ? 16 : 32;
-    p.tensor = false;
+    p.rows = rows <= 16 ? 16 : (rows <= 32 ? 32 : 256);
     p.tiles = (int)((rows + p.rows - 1) / p.rows);
     const long long units = (long long)B * kv_heads * p.tiles;
-    long long s = (long long)rows_ctas_per_sm(p.rows) * sms / units;
-    const long long most = (max_keys + 127) / 128;                       // two chunks for each of a CTA's warps
+    long long s = (long long)ctas_per_sm(p.rows) * sms / units;
+    // two chunks for each of a CTA's warps, two steps of the tensor-memory kernel
+    const long long most = p.rows == 256 ? (max_keys + 255) / 256 : (max_keys + 127) / 128;
     if (s > most) s = most;
     p.slices = (int)(s < 1 ? 1 : s);
     return p;
 }
 
 // Enough for any call: there are several slices only where all row tiles' slices together are resident at once.
-size_t kv8_partial_bytes(int dim, int sms) { return (size_t)sms * rows_ctas_per_sm(32) * 32 * (dim * 4 + 8); }
+size_t kv8_partial_bytes(int dim, int sms) { return (size_t)sms * 256 * (dim * 4 + 8); }
 
 cudaError_t launch_kv8_attention(const w4a8_kv8_cache& c, const void* q, long long q_stride, int B, int T, int q_heads, const int32_t* table,
                                  int table_width, const int32_t* limits, float scale, void* out, void* workspace, cudaStream_t stream) {
-    const Kv8Plan p = kv8_plan(B, T, q_heads, c.heads, c.dim, (long long)table_width * c.block, device_sm_count());
+    const Kv8Plan p = kv8_plan(B, T, q_heads, c.heads, (long long)table_width * c.block, device_sm_count());
     AttendArgs a;
     a.k_codes = c.k_codes;
     a.v_codes = c.v_codes;
@@ -494,7 +494,9 @@ cudaError_t launch_kv8_attention(const w4a8_kv8_cache& c, const void* q, long lo
     a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + WS_SHARED_OFF);
     a.part_ml = reinterpret_cast<float2*>(a.part_o + units * p.rows * c.dim);
     cudaError_t e;
-    if (p.rows == 16)
+    if (p.rows == 256)
+        e = launch_kv8_tiles(a, B, c.dim, stream);
+    else if (p.rows == 16)
         e = c.dim == 128 ? launch_rows<128, 1>(a, B, stream) : launch_rows<64, 1>(a, B, stream);
     else
         e = c.dim == 128 ? launch_rows<128, 2>(a, B, stream) : launch_rows<64, 2>(a, B, stream);

@@ -81,12 +81,13 @@ __device__ __forceinline__ uint32_t kv8_pack_half2(float lo, float hi) {
     return r;
 }
 
-// Which kernel, how many rows per tile and how many slices of the keys (w4a8_kv8_attention and its workspace size).
+// Which kernel, how many rows per tile and how many slices of the keys.
 struct Kv8Plan {
-    int rows;                           // rows per tile
+    int rows;                           // rows per tile: 16, 32, or TC_ROWS for the tensor-memory kernel
     int tiles, slices;
-    bool tensor;                        // the tcgen05 kernel
 };
-Kv8Plan kv8_plan(int B, int T, int q_heads, int kv_heads, int dim, long long max_keys, int sms);
+Kv8Plan kv8_plan(int B, int T, int q_heads, int kv_heads, long long max_keys, int sms);
+
+cudaError_t launch_kv8_tiles(const AttendArgs& a, int B, int dim, cudaStream_t stream);      // 256 rows per tile
 
 }  // namespace w4a8

@@ -1,0 +1,450 @@
+// Attention over the 8-bit key/value cache for many rows: chunks of new tokens, prompts (definition and number formats in
+// kv8_attention.cuh).  The 5th-generation tensor cores take fp16 operands, so the codes are made fp16 on their way into shared
+// memory, once for the 256 rows of a CTA.
+//
+// One CTA per (sequence, key head, tile of 256 rows, slice of the keys), 128 positions a step, two halves of 128 rows in turn:
+//   S_h = Q_h K^T         both operands in shared memory (K-major, 128-byte swizzle), sums in tensor memory
+//   O_h += W_h V          W_h = the weights, fp16, in tensor memory over the scores they came from; V [position][channel] as it is in
+//                         the cache (an MN-major operand: nothing is transposed)
+// While one half's products run, the other half's weights are formed.  Warps: two groups of four form the weights, a thread per row (the
+// lane of tensor memory that it may read is its row); four convert codes, straight from global memory through registers (each
+// 16-byte piece is read by one thread once, so nothing would be gained by a copy into shared memory first); one issues the products.
+// All waits are bounded: a role that gives up sets the CTA's abort flag, on which the others leave, too.
+//
+// A step's products cost 2 x 128 x 128 x D x 2 multiply-adds (2048 cycles of the tensor pipe at D = 128), its 32768 exponentials as much of the
+// special-function units, its operands and the conversion as much of shared memory's bandwidth: none of the three bounds it alone.
+#include "kv8_attention.cuh"
+
+namespace w4a8 {
+namespace {
+
+constexpr int TC_THREADS = 512, TC_ROWS = 256, TC_KEYS = 128;
+constexpr int TC_WARP_CVT0 = 8, TC_WARP_MMA = 12;
+constexpr int TC_META = 4;                                    // ring of the steps' block scales
+
+template <int D>
+struct TcCfg {
+    static constexpr int PANEL = 128 * 128;                   // 128 rows of 64 halves
+    static constexpr int PANELS = D / 64;
+    static constexpr int TILE = PANEL * PANELS;
+    static constexpr int Q_OFF = 0, K_OFF = 2 * TILE, V_OFF = 4 * TILE;
+    static constexpr int BAR_OFF = 6 * TILE;
+    // barriers: K and V stages full and empty, scores and weights of a half, Q of a half, O of a half complete, scales, end
+    static constexpr int KF = 0, KE = 2, VF = 4, VE = 6, SF = 8, PF = 10, QF = 12, OF = 14, MF = 16, FINAL = MF + TC_META, NUM_BARS = FINAL + 1;
+    static constexpr int META_OFF = (BAR_OFF + NUM_BARS * 8 + 15) & ~15;        // [TC_META][8] float4: key scale, log2 of the value scale, its reciprocal
+    static constexpr int MISC_OFF = META_OFF + TC_META * 8 * 16;                // tensor-memory base, abort flag, longest limit
+    static constexpr int SMEM = MISC_OFF + 16 + 1024;
+    static constexpr uint32_t S_COL = 0, O_COL = 256;                            // tensor memory: scores 2 x 128 columns, sums 2 x 128
+};
+
+template <int D>
+__global__ void __launch_bounds__(TC_THREADS, 1)
+kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
+    using C = TcCfg<D>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* smem = smem_raw + (base - ptx::smem_u32(smem_raw));
+    const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
+    ptx::pdl_launch_dependents();
+    auto bar = [&](int i) { return base + C::BAR_OFF + 8 * i; };
+    volatile uint32_t* tmem_holder = reinterpret_cast<volatile uint32_t*>(smem + C::MISC_OFF);
+    volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + C::MISC_OFF + 4);
+    int* longest_at = reinterpret_cast<int*>(smem + C::MISC_OFF + 8);
+    if (warp == TC_WARP_MMA) {
+        if (lane == 0) {
+            *abort_flag = 0;
+            *longest_at = 0;
+            for (int i = 0; i < 2; ++i) {
+                ptx::mbar_init(bar(C::KF + i), 4);
+                ptx::mbar_init(bar(C::KE + i), 1);
+                ptx::mbar_init(bar(C::VF + i), 4);
+                ptx::mbar_init(bar(C::VE + i), 1);
+                ptx::mbar_init(bar(C::SF + i), 1);
+                ptx::mbar_init(bar(C::PF + i), 4);
+                ptx::mbar_init(bar(C::QF + i), 4);
+                ptx::mbar_init(bar(C::OF + i), 1);
+            }
+            for (int i = 0; i < TC_META; ++i) ptx::mbar_init(bar(C::MF + i), 1);
+            ptx::mbar_init(bar(C::FINAL), 1);
+            ptx::fence_mbar_init();
+        }
+        __syncwarp();
+        ptx::tmem_alloc(base + C::MISC_OFF, 512);
+        ptx::tmem_relinquish();
+    }
+    // late tiles first: under a causal limit they are the longest
+    const int units = gridDim.x / (a.tiles * a.slices);
+    const int ts = blockIdx.x / units, unit = blockIdx.x - ts * units;
+    const int tile = a.tiles - 1 - ts / a.slices, slice = ts % a.slices;
+    const int seq = unit / a.kv_heads, kv_head = unit - seq * a.kv_heads;
+    const int rows = a.T * a.rep, row0 = tile * TC_ROWS;
+    const int halves = rows - row0 > 128 ? 2 : 1;
+    const int capacity = (int)min((long long)a.table_width << a.log2_block, 0x7FFFFF00ll);
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem = *tmem_holder;
+    ptx::pdl_wait();
+
+    int limit = 0, token = 0, head = 0;
+    const int row = row0 + tid;                               // threads 0..255: this thread's row
+    if (tid < TC_ROWS && row < rows) {
+        token = row / a.rep;
+        head = kv_head * a.rep + row - token * a.rep;
+        limit = min(max(__ldcg(a.limits + (long long)seq * a.T + token), 0), capacity);
+    }
+    if (tid < TC_ROWS) {
+        const int top = __reduce_max_sync(0xFFFFFFFFu, limit);
+        if (lane == 0 && top) atomicMax(longest_at, top);
+    }
+    __syncthreads();
+    const int longest = *longest_at;
+    const int tiles_n = (int)(((long long)longest + TC_KEYS - 1) / TC_KEYS);
+    const int t_lo = (int)((long long)slice * tiles_n / a.slices), n = (int)((long long)(slice + 1) * tiles_n / a.slices) - t_lo;
+
+    if (warp < TC_WARP_CVT0) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+        const int h = warp >> 2;
+        if (h < halves) {
+            // ---- this thread's row of q, scaled by a power of two and rounded to fp16, into the half's operand tile
+            float factor;
+            {
+                uint32_t w[D / 2];
+                uint32_t run = 0;
+                if (row < rows) {
+                    const uint4* src = reinterpret_cast<const uint4*>(a.q + ((long long)seq * a.T + token) * a.q_stride + (long long)head * D);
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) {
+                        const uint4 x = __ldcg(src + i);
+                        w[4 * i] = x.x, w[4 * i + 1] = x.y, w[4 * i + 2] = x.z, w[4 * i + 3] = x.w;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < D / 2; ++i) w[i] = 0;
+                }
+#pragma unroll
+                for (int i = 0; i < D / 2; ++i) run = __vmaxu2(run, w[i] & 0x7FFF7FFFu);
+                const int e = kv8_row_exp(max(run & 0xFFFFu, run >> 16));
+                const float up = kv8_pow2(e);
+                factor = a.scale_log2 * kv8_pow2(-e);
+                const int r = tid & 127;
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) {
+                    uint32_t x[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        x[k] = kv8_pack_half2(__uint_as_float(w[4 * i + k] << 16) * up, __uint_as_float(w[4 * i + k] & 0xFFFF0000u) * up);
+                    ptx::sts128u(base + C::Q_OFF + h * C::TILE + (i >> 3) * C::PANEL + r * 128 + (((i & 7) ^ (r & 7)) << 4), x[0], x[1], x[2], x[3]);
+                }
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(bar(C::QF + h));
+            }
+            const int shortest = __reduce_min_sync(0xFFFFFFFFu, row < rows ? limit : 0x7FFFFFFF);
+            const uint32_t lanes = (uint32_t)(warp & 3) << 21;                  // tensor-memory lanes of this warp
+            const uint32_t s_col = tmem + lanes + C::S_COL + h * 128, o_col = tmem + lanes + C::O_COL + h * 128;
+            float ref = -INFINITY, sum = 0.0f;
+            bool ok = true;
+            for (int j = 0; j < n; ++j) {
+                if (!(ok = ptx::warp_mbar_wait_suspend(bar(C::MF + j % TC_META), (j / TC_META) & 1, abort_flag))) break;
+                if (!(ok = ptx::warp_mbar_wait_suspend(bar(C::SF + h), j & 1, abort_flag))) break;
+                ptx::tc_fence_after_sync();
+                uint32_t s[4][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(s_col + 32 * c, s[c]);
+                const uint32_t meta = base + C::META_OFF + (j % TC_META) * 128;
+                const int key0 = (t_lo + j) * TC_KEYS;
+                float off = ref == -INFINITY ? 0.0f : KV8_W_EXP - ref;
+                ptx::tmem_ld_wait();
+                float top = -INFINITY;
+#pragma unroll
+                for (int b = 0; b < 8; ++b) {
+                    const uint4 m = ptx::lds128(meta + 16 * b);
+                    const float f = factor * __uint_as_float(m.x), add = __uint_as_float(m.y) + off;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        uint32_t& v = s[b >> 1][(b & 1) * 16 + i];
+                        v = __float_as_uint(fmaf(__uint_as_float(v), f, add));
+                    }
+                }
+                if (key0 + TC_KEYS > shortest) {
+#pragma unroll
+                    for (int i = 0; i < 128; ++i)
+                        if (key0 + i >= limit) s[i >> 5][i & 31] = __float_as_uint(-INFINITY);
+                }
+#pragma unroll
+                for (int i = 0; i < 128; i += 2) top = fmaxf(top, fmaxf(__uint_as_float(s[i >> 5][i & 31]), __uint_as_float(s[i >> 5][(i + 1) & 31])));
+                const bool past = top > (ref == -INFINITY ? -INFINITY : KV8_W_EXP + KV8_SLACK);
+                if (__any_sync(0xFFFFFFFFu, past)) {
+                    // (a step's scores are complete only when the products of the step before are: O is at rest)
+                    float f = 1.0f, shift = 0.0f;
+                    if (past) {
+                        const float now = top - off;
+                        f = ref == -INFINITY ? 0.0f : kv8_ex2(ref - now);
+                        ref = now;
+                        shift = KV8_W_EXP - ref - off;
+                        sum *= f;
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 128; ++i) s[i >> 5][i & 31] = __float_as_uint(__uint_as_float(s[i >> 5][i & 31]) + shift);
+                    if (j > 0) {
+#pragma unroll
+                        for (int c = 0; c < D; c += 16) {
+                            uint32_t o[16];
+                            ptx::tmem_ld_32x16(o_col + c, o);
+                            ptx::tmem_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            ptx::tmem_st_32x8(o_col + c, o[0], o[1], o[2], o[3], o[4], o[5], o[6], o[7]);
+                            ptx::tmem_st_32x8(o_col + c + 8, o[8], o[9], o[10], o[11], o[12], o[13], o[14], o[15]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t p[32];
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        float g0 = 0.0f, g1 = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int at = (4 * c + b) * 16 + 2 * i;
+                            const float w0 = kv8_ex2(__uint_as_float(s[at >> 5][at & 31])), w1 = kv8_ex2(__uint_as_float(s[at >> 5][(at + 1) & 31]));
+                            g0 += w0;
+                            g1 += w1;
+                            p[b * 8 + i] = kv8_pack_half2(w0, w1);
+                        }
+                        sum = fmaf(g0 + g1, __uint_as_float(ptx::lds32(meta + 16 * (4 * c + b) + 8)), sum);
+                    }
+                    ptx::tmem_st_32x32(s_col + 32 * c, p);
+                }
+                ptx::tmem_st_wait();
+                ptx::tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(bar(C::PF + h));
+            }
+            // ---- this thread's row of the result
+            if (ok && n > 0) ok = ptx::warp_mbar_wait_suspend(bar(C::OF + h), 0, abort_flag);
+            if (ok) {
+                ptx::tc_fence_after_sync();
+                const float inv = sum == 0.0f ? 0.0f : __fdividef(1.0f, sum);
+                const size_t part = (((size_t)unit * a.tiles + tile) * a.slices + slice) * TC_ROWS + (size_t)(row - row0);
+                uint16_t* dst = a.out + (((long long)seq * a.T + token) * a.q_heads + head) * D;
+#pragma unroll
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t o[32];
+                    if (n > 0) {
+                        ptx::tmem_ld_32x32(o_col + c, o);
+                        ptx::tmem_ld_wait();
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = 0;
+                    }
+                    if (row < rows && a.slices > 1) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4)
+                            *reinterpret_cast<uint4*>(a.part_o + part * D + c + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                    } else if (row < rows) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) {
+                            uint32_t y[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                y[k] = ptx::pack_bf16x2(__uint_as_float(o[i + 2 * k]) * inv, __uint_as_float(o[i + 2 * k + 1]) * inv);
+                            *reinterpret_cast<uint4*>(dst + c + i) = make_uint4(y[0], y[1], y[2], y[3]);
+                        }
+                    }
+                    __syncwarp();                            // ahead of the next load of tensor memory
+                }
+                if (a.slices > 1 && row < rows) a.part_ml[part] = make_float2(ref, sum);
+            }
+        }
+    } else if (warp < TC_WARP_MMA) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+        // ---- codes -> fp16 operand tiles.  A thread takes 16 codes of a key at a time; eight neighbouring lanes take the same piece of eight
+        // keys, whose swizzled places differ, so that the stores touch all banks once.
+        constexpr int L = D / 16;                             // pieces per thread and tile
+        const int wv = warp - TC_WARP_CVT0, r8 = lane & 7, p8 = lane >> 3;
+        const int32_t* table = a.table + (size_t)seq * a.table_width;
+        // lane l: block number of positions 16 (l & 7) .. + 15 of a tile
+        auto number_of = [&](int j) -> int {
+            const long long pos = (long long)(t_lo + j) * TC_KEYS + 16 * r8;
+            if (j >= n || pos >= longest) return -1;
+            const int number = __ldcg(table + (pos >> a.log2_block));
+            if ((unsigned)number < (unsigned)a.num_blocks) return number;
+            *a.status = W4A8_ERR_INDEX;
+            return -1;
+        };
+        auto group_of = [&](int i) { return D == 128 ? (i >> 1) * 4 + wv : i * 4 + wv; };        // which eight keys of the tile
+        auto piece_of = [&](int i) { return D == 128 ? p8 + 4 * (i & 1) : p8; };
+        auto load = [&](uint4 (&x)[L], const int8_t* codes, int number, int j) {
+#pragma unroll
+            for (int i = 0; i < L; ++i) {
+                const int key = group_of(i) * 8 + r8;
+                const int b = __shfl_sync(0xFFFFFFFFu, number, group_of(i) >> 1);
+                const int slot = ((t_lo + j) * TC_KEYS + key) & ((1 << a.log2_block) - 1);
+                x[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (b >= 0) x[i] = __ldcg(reinterpret_cast<const uint4*>(codes + ((((size_t)b * a.kv_heads + kv_head) << a.log2_block) + slot) * D + piece_of(i) * 16));
+            }
+        };
+        auto store = [&](const uint4 (&x)[L], uint32_t dst) {
+#pragma unroll
+            for (int i = 0; i < L; ++i) {
+                const int p = piece_of(i);
+                const uint32_t at = dst + (p >> 2) * C::PANEL + (group_of(i) * 8 + r8) * 128;
+                const uint32_t w[4] = {x[i].x ^ 0x80808080u, x[i].y ^ 0x80808080u, x[i].z ^ 0x80808080u, x[i].w ^ 0x80808080u};
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    ptx::sts128u(at + (((2 * (p & 3) + k) ^ r8) << 4), kv8_half2(w[2 * k], 0x4140), kv8_half2(w[2 * k], 0x4342),
+                                 kv8_half2(w[2 * k + 1], 0x4140), kv8_half2(w[2 * k + 1], 0x4342));
+            }
+        };
+        uint4 k[L], v[L];
+        int number = number_of(0), next = number_of(1);
+        uint32_t ks = 0, vs = 0;
+        auto scales = [&](int b) {
+            ks = vs = 0;
+            if (wv == 0 && lane < 8 && b >= 0) {
+                ks = __ldcg(a.k_scales + (size_t)b * a.kv_heads + kv_head);
+                vs = __ldcg(a.v_scales + (size_t)b * a.kv_heads + kv_head);
+            }
+        };
+        if (n > 0) {
+            load(k, a.k_codes, number, 0);
+            load(v, a.v_codes, number, 0);
+            scales(number);
+        }
+        for (int j = 0; j < n; ++j) {
+            const int st = j & 1;
+            const uint32_t parity = ((j >> 1) & 1) ^ 1;
+            if (!ptx::warp_mbar_wait_suspend(bar(C::KE + st), parity, abort_flag)) break;
+            if (wv == 0) {
+                // a stage is free when its scores are complete, and those follow the weights of the step before: this slot's are used
+                if (lane < 8) {
+                    float lg, inv;
+                    kv8_value_scale(vs, lg, inv);
+                    if (number < 0) lg = -INFINITY, inv = 0.0f;
+                    ptx::sts128(base + C::META_OFF + (j % TC_META) * 128 + lane * 16, make_float4(__half2float(__ushort_as_half((uint16_t)ks)), lg, inv, 0.0f));
+                }
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(bar(C::MF + j % TC_META));
+            }
+            store(k, base + C::K_OFF + st * C::TILE);
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(bar(C::KF + st));
+            number = next;
+            load(k, a.k_codes, number, j + 1);
+            scales(number);
+            next = number_of(j + 2);
+            if (!ptx::warp_mbar_wait_suspend(bar(C::VE + st), parity, abort_flag)) break;
+            store(v, base + C::V_OFF + st * C::TILE);
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(bar(C::VF + st));
+            load(v, a.v_codes, number, j + 1);
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (warp == TC_WARP_MMA && n > 0) {
+            // ---- products: the warp walks the loop, one elected lane issues
+            const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
+            constexpr uint32_t IDESC_S = ptx::idesc_f16(128, TC_KEYS, false), IDESC_O = ptx::idesc_f16(128, D, true);
+            auto scores = [&](int h, int st) {
+                const uint64_t q0 = ptx::smem_desc_k_sw128(base + C::Q_OFF + h * C::TILE), k0 = ptx::smem_desc_k_sw128(base + C::K_OFF + st * C::TILE);
+                if (ptx::elect_one()) {
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) {
+                        const uint64_t at = (uint64_t)((i >> 2) * (C::PANEL / 16) + (i & 3) * 2);
+                        ptx::mma_f16_ss(tm + C::S_COL + h * 128, q0 + at, k0 + at, IDESC_S, i > 0);
+                    }
+                    ptx::tc_commit(bar(C::SF + h));
+                    if (h == halves - 1) ptx::tc_commit(bar(C::KE + st));
+                }
+                __syncwarp();
+            };
+            bool ok = true;
+            for (int h = 0; h < halves && ok; ++h) {
+                ok = ptx::mbar_wait_suspend(bar(C::QF + h), 0, abort_flag);
+                if (ok && h == 0) ok = ptx::mbar_wait_suspend(bar(C::KF), 0, abort_flag);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (ok) {
+                    ptx::tc_fence_after_sync();
+                    scores(h, 0);
+                }
+            }
+            for (int j = 0; j < n && ok; ++j) {
+                const int st = j & 1;
+                for (int h = 0; h < halves && ok; ++h) {
+                    if (h == 0) ok = ptx::mbar_wait_suspend(bar(C::VF + st), (j >> 1) & 1, abort_flag);
+                    ok = ok && ptx::mbar_wait_suspend(bar(C::PF + h), j & 1, abort_flag);
+                    ok = __all_sync(0xFFFFFFFFu, ok);
+                    if (!ok) break;
+                    ptx::tc_fence_after_sync();
+                    const uint64_t v0 = ptx::smem_desc_mn_sw128(base + C::V_OFF + st * C::TILE, C::PANEL);
+                    if (ptx::elect_one()) {
+#pragma unroll
+                        for (int i = 0; i < TC_KEYS / 16; ++i)
+                            ptx::mma_f16_ts(tm + C::O_COL + h * 128, tm + C::S_COL + h * 128 + 8 * i, v0 + (uint64_t)(i * 128), IDESC_O, j > 0 || i > 0);
+                        if (h == halves - 1) ptx::tc_commit(bar(C::VE + st));
+                        if (j == n - 1) ptx::tc_commit(bar(C::OF + h));
+                    }
+                    __syncwarp();
+                    if (j + 1 < n) {
+                        if (h == 0) ok = ptx::mbar_wait_suspend(bar(C::KF + (st ^ 1)), ((j + 1) >> 1) & 1, abort_flag);
+                        ok = __all_sync(0xFFFFFFFFu, ok);
+                        if (!ok) break;
+                        ptx::tc_fence_after_sync();
+                        scores(h, st ^ 1);
+                    }
+                }
+            }
+            if (ptx::elect_one()) ptx::tc_commit(bar(C::FINAL));
+            __syncwarp();
+            ptx::mbar_wait(bar(C::FINAL), 0, abort_flag);    // nothing may still be executing when tensor memory is freed
+        }
+    }
+    if (*abort_flag && lane == 0) atomicExch(a.status, (uint32_t)W4A8_ERR_TIMEOUT);
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    if (warp == TC_WARP_MMA) {
+        ptx::tc_fence_after_sync();
+        ptx::tmem_dealloc(tmem, 512);
+    }
+}
+
+template <int D>
+cudaError_t launch_tiles(const AttendArgs& a, int B, cudaStream_t stream) {
+    using C = TcCfg<D>;
+    static_assert(C::SMEM <= 227 * 1024, "shared memory");
+    static bool ready[64] = {false};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (!ready[dev]) {
+        e = cudaFuncSetAttribute(kv8_attend_tiles_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+        if (e != cudaSuccess) return e;
+        ready[dev] = true;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)a.tiles * (unsigned)a.slices * (unsigned)(B * a.kv_heads), 1, 1);
+    cfg.blockDim = dim3(TC_THREADS, 1, 1);
+    cfg.dynamicSmemBytes = C::SMEM;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kv8_attend_tiles_kernel<D>, a);
+}
+
+}  // namespace
+
+cudaError_t launch_kv8_tiles(const AttendArgs& a, int B, int dim, cudaStream_t stream) {
+    return dim == 128 ? launch_tiles<128>(a, B, stream) : launch_tiles<64>(a, B, stream);
+}
+
+}  // namespace w4a8

@@ -165,10 +165,27 @@ __device__ __forceinline__ bool mbar_wait_limit(uint32_t bar, uint32_t parity, v
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag) {
     return mbar_wait_limit(bar, parity, abort_flag, WAIT_LIMIT_NS);
 }
+// Same contract, by try_wait alone (the hardware suspends the thread for as long as it sees fit): between the two above, for waits of
+// some hundred cycles on the critical path with other warps at work beside them.
+__device__ __forceinline__ bool mbar_wait_suspend(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag) {
+    uint64_t t0 = 0;
+    for (uint32_t spin = 1;; ++spin) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((spin & 0x3F) == 0) {
+            if (*abort_flag) return false;
+            const uint64_t now = globaltimer_ns();
+            if (t0 == 0) t0 = now;
+            else if (now - t0 > WAIT_LIMIT_NS) { *abort_flag = 1; return false; }
+        }
+    }
+}
 // The same for a whole warp, converged, ahead of warp-collective instructions (tcgen05.ld, tcgen05.st): the lanes leave together and
 // with one outcome, also when the phase completes between their probes or the wait runs out for some of them.
 __device__ __forceinline__ bool warp_mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag) {
     return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag));
+}
+__device__ __forceinline__ bool warp_mbar_wait_suspend(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag) {
+    return __all_sync(0xFFFFFFFFu, mbar_wait_suspend(bar, parity, abort_flag));
 }
 __device__ __forceinline__ bool warp_mbar_wait_hot(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag) {
     return __all_sync(0xFFFFFFFFu, mbar_wait_hot(bar, parity, abort_flag));
@@ -365,6 +382,22 @@ __device__ __forceinline__ void mma_i8_ts(uint32_t d_tmem, uint32_t a_tmem, uint
         "tcgen05.mma.cta_group::1.kind::i8 [%0], [%1], %2, %3, p;\n\t}"
         ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
+// fp16 operands, fp32 sums: A and B from shared memory (one K = 16 step), and A (128 rows = TMEM lanes, 8 columns of two halves per
+// step) from tensor memory
+__device__ __forceinline__ void mma_f16_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
 // arrive on an mbarrier once every tcgen05 op issued so far by this thread has completed
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -404,6 +437,17 @@ __device__ __forceinline__ void tmem_st_32x8(uint32_t taddr, uint32_t r0, uint32
         "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
         ::"r"(taddr), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(r4), "r"(r5), "r"(r6), "r"(r7) : "memory");
 }
+// ... 32 registers, 32 consecutive columns
+__device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+          "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+          "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() {
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
@@ -421,6 +465,18 @@ __device__ __forceinline__ uint64_t smem_desc_k_sw128(uint32_t addr) {
     d |= (uint64_t)(1024 >> 4) << 32;                  // [32,46) stride byte offset >> 4
     d |= (uint64_t)1 << 46;                            // [46,48) descriptor version (sm_100)
     d |= (uint64_t)2 << 61;                            // [61,64) layout: 128-byte swizzle
+    return d;
+}
+
+// MN-major operand of 16-bit elements, 128-byte swizzle: rows of 64 elements of the M or N range (128 bytes), one row per k, eight rows
+// to a swizzle atom, atoms 1024 B apart along k; `panel` bytes from 64 elements to the next 64.  A K = 16 step is two atoms.
+__device__ __forceinline__ uint64_t smem_desc_mn_sw128(uint32_t addr, uint32_t panel) {
+    uint64_t d = 0;
+    d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(panel >> 4) << 16;                 // leading byte offset: to the next 64 elements
+    d |= (uint64_t)(1024 >> 4) << 32;                  // stride byte offset: to the next eight k
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
     return d;
 }
 
@@ -443,6 +499,14 @@ __host__ __device__ constexpr uint32_t idesc_i8(int mma_m, int mma_n, bool a_sig
          | (0u << 15) | (0u << 16)           // A, B K-major
          | ((uint32_t)(mma_n >> 3) << 17)    // [17,23) N / 8
          | ((uint32_t)(mma_m >> 4) << 24);   // [24,29) M / 16
+}
+
+// Instruction descriptor for kind::f16: fp16 A (K-major) and B, fp32 accumulator.
+__host__ __device__ constexpr uint32_t idesc_f16(int mma_m, int mma_n, bool b_mn_major) {
+    return (1u << 4)                         // [4,6)   D format: F32
+         | (0u << 7) | (0u << 10)            // A, B format: F16
+         | ((b_mn_major ? 1u : 0u) << 16)    // B major
+         | ((uint32_t)(mma_n >> 3) << 17) | ((uint32_t)(mma_m >> 4) << 24);
 }
 
 }  // namespace ptx
