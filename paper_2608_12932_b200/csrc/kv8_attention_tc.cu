@@ -7,8 +7,9 @@
 //   O_h += W_h V          W_h = the weights, fp16, in tensor memory over the scores they came from; V [position][channel] as it is in
 //                         the cache (an MN-major operand: nothing is transposed)
 // While one half's products run, the other half's weights are formed.  Warps: two groups of four form the weights, a thread per row (the
-// lane of tensor memory that it may read is its row); four convert codes, straight from global memory through registers (each
-// 16-byte piece is read by one thread once, so nothing would be gained by a copy into shared memory first); one issues the products.
+// lane of tensor memory that it may read is its row); four convert codes; one fetches them with bulk copies, 64 positions of K or V at a time,
+// into a ring ahead of the conversion (loads through the converting threads' registers instead: a causal prompt of 4096 in 252 us);
+// one issues the products.
 // All waits are bounded: a role that gives up sets the CTA's abort flag, on which the others leave, too.
 //
 // A step's products cost 2 x 128 x 128 x D x 2 multiply-adds (2048 cycles of the tensor pipe at D = 128), its 32768 exponentials as much of the
@@ -19,8 +20,8 @@ namespace w4a8 {
 namespace {
 
 constexpr int TC_THREADS = 512, TC_ROWS = 256, TC_KEYS = 128;
-constexpr int TC_WARP_CVT0 = 8, TC_WARP_MMA = 12;
-constexpr int TC_META = 4;                                    // ring of the steps' block scales
+constexpr int TC_WARP_CVT0 = 8, TC_WARP_MMA = 12, TC_WARP_FETCH = 13;
+constexpr int TC_META = 8;                                    // ring of the steps' block scales
 
 template <int D>
 struct TcCfg {
@@ -28,9 +29,12 @@ struct TcCfg {
     static constexpr int PANELS = D / 64;
     static constexpr int TILE = PANEL * PANELS;
     static constexpr int Q_OFF = 0, K_OFF = 2 * TILE, V_OFF = 4 * TILE;
-    static constexpr int BAR_OFF = 6 * TILE;
-    // barriers: K and V stages full and empty, scores and weights of a half, Q of a half, O of a half complete, scales, end
-    static constexpr int KF = 0, KE = 2, VF = 4, VE = 6, SF = 8, PF = 10, QF = 12, OF = 14, MF = 16, FINAL = MF + TC_META, NUM_BARS = FINAL + 1;
+    static constexpr int RAW = 64 * D, SLOTS = D == 128 ? 4 : 8;  // codes of 64 positions; K, K, V, V of a step in turn
+    static constexpr int RAW_OFF = 6 * TILE;
+    static constexpr int BAR_OFF = RAW_OFF + SLOTS * RAW;
+    // barriers: K and V stages full and empty, scores and weights of a half, Q of a half, O of a half complete, scales, raw codes full and
+    // empty, end
+    static constexpr int KF = 0, KE = 2, VF = 4, VE = 6, SF = 8, PF = 10, QF = 12, OF = 14, MF = 16, RF = MF + TC_META, RE = RF + SLOTS, FINAL = RE + SLOTS, NUM_BARS = FINAL + 1;
     static constexpr int META_OFF = (BAR_OFF + NUM_BARS * 8 + 15) & ~15;        // [TC_META][8] float4: key scale, log2 of the value scale, its reciprocal
     static constexpr int MISC_OFF = META_OFF + TC_META * 8 * 16;                // tensor-memory base, abort flag, longest limit
     static constexpr int SMEM = MISC_OFF + 16 + 1024;
@@ -65,6 +69,10 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
                 ptx::mbar_init(bar(C::OF + i), 1);
             }
             for (int i = 0; i < TC_META; ++i) ptx::mbar_init(bar(C::MF + i), 1);
+            for (int i = 0; i < C::SLOTS; ++i) {
+                ptx::mbar_init(bar(C::RF + i), 1);
+                ptx::mbar_init(bar(C::RE + i), 4);
+            }
             ptx::mbar_init(bar(C::FINAL), 1);
             ptx::fence_mbar_init();
         }
@@ -103,7 +111,7 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
     const int t_lo = (int)((long long)slice * tiles_n / a.slices), n = (int)((long long)(slice + 1) * tiles_n / a.slices) - t_lo;
 
     if (warp < TC_WARP_CVT0) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         const int h = warp >> 2;
         if (h < halves) {
             // ---- this thread's row of q, scaled by a power of two and rounded to fp16, into the half's operand tile
@@ -261,89 +269,47 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
             }
         }
     } else if (warp < TC_WARP_MMA) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-        // ---- codes -> fp16 operand tiles.  A thread takes 16 codes of a key at a time; eight neighbouring lanes take the same piece of eight
-        // keys, whose swizzled places differ, so that the stores touch all banks once.
-        constexpr int L = D / 16;                             // pieces per thread and tile
-        const int wv = warp - TC_WARP_CVT0, r8 = lane & 7, p8 = lane >> 3;
-        const int32_t* table = a.table + (size_t)seq * a.table_width;
-        // lane l: block number of positions 16 (l & 7) .. + 15 of a tile
-        auto number_of = [&](int j) -> int {
-            const long long pos = (long long)(t_lo + j) * TC_KEYS + 16 * r8;
-            if (j >= n || pos >= longest) return -1;
-            const int number = __ldcg(table + (pos >> a.log2_block));
-            if ((unsigned)number < (unsigned)a.num_blocks) return number;
-            *a.status = W4A8_ERR_INDEX;
-            return -1;
-        };
-        auto group_of = [&](int i) { return D == 128 ? (i >> 1) * 4 + wv : i * 4 + wv; };        // which eight keys of the tile
-        auto piece_of = [&](int i) { return D == 128 ? p8 + 4 * (i & 1) : p8; };
-        auto load = [&](uint4 (&x)[L], const int8_t* codes, int number, int j) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        // ---- codes -> fp16 operand tiles, 16 codes (a piece) of a key at a time.  Eight neighbouring lanes take eight different pieces
+        // of 128 bytes, of two keys, so that neither the reads nor the stores (whose places are swizzled by the key) meet in a bank.
+        constexpr int L = D / 32;                             // pieces per thread and 64 positions
+        const int wv = warp - TC_WARP_CVT0;
+        const int piece = D == 128 ? lane & 7 : lane & 3;
+        const int key0 = wv * 16 + (D == 128 ? ((lane >> 4) & 1) * 2 + (((lane >> 2) ^ (lane >> 3)) & 1) : lane >> 2);
+        constexpr int STEP = D == 128 ? 4 : 8;                // keys from one piece of a thread to its next
+        const uint32_t from = key0 * D + piece * 16;
+        const uint32_t to = (piece >> 2) * C::PANEL + key0 * 128 + (((2 * (piece & 3)) ^ (key0 & 7)) << 4);
+        auto convert = [&](uint32_t src, uint32_t dst) {
+            uint4 x[L];
+#pragma unroll
+            for (int i = 0; i < L; ++i) x[i] = ptx::lds128(src + from + i * STEP * D);
 #pragma unroll
             for (int i = 0; i < L; ++i) {
-                const int key = group_of(i) * 8 + r8;
-                const int b = __shfl_sync(0xFFFFFFFFu, number, group_of(i) >> 1);
-                const int slot = ((t_lo + j) * TC_KEYS + key) & ((1 << a.log2_block) - 1);
-                x[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (b >= 0) x[i] = __ldcg(reinterpret_cast<const uint4*>(codes + ((((size_t)b * a.kv_heads + kv_head) << a.log2_block) + slot) * D + piece_of(i) * 16));
-            }
-        };
-        auto store = [&](const uint4 (&x)[L], uint32_t dst) {
-#pragma unroll
-            for (int i = 0; i < L; ++i) {
-                const int p = piece_of(i);
-                const uint32_t at = dst + (p >> 2) * C::PANEL + (group_of(i) * 8 + r8) * 128;
                 const uint32_t w[4] = {x[i].x ^ 0x80808080u, x[i].y ^ 0x80808080u, x[i].z ^ 0x80808080u, x[i].w ^ 0x80808080u};
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    ptx::sts128u(at + (((2 * (p & 3) + k) ^ r8) << 4), kv8_half2(w[2 * k], 0x4140), kv8_half2(w[2 * k], 0x4342),
-                                 kv8_half2(w[2 * k + 1], 0x4140), kv8_half2(w[2 * k + 1], 0x4342));
+                const uint32_t at = (dst + to + i * STEP * 128) ^ (D == 128 && (i & 1) ? 64u : 0u);      // (four keys on: bit 2 of the swizzle)
+                ptx::sts128u(at, kv8_half2(w[0], 0x4140), kv8_half2(w[0], 0x4342), kv8_half2(w[1], 0x4140), kv8_half2(w[1], 0x4342));
+                ptx::sts128u(at ^ 16u, kv8_half2(w[2], 0x4140), kv8_half2(w[2], 0x4342), kv8_half2(w[3], 0x4140), kv8_half2(w[3], 0x4342));
             }
         };
-        uint4 k[L], v[L];
-        int number = number_of(0), next = number_of(1);
-        uint32_t ks = 0, vs = 0;
-        auto scales = [&](int b) {
-            ks = vs = 0;
-            if (wv == 0 && lane < 8 && b >= 0) {
-                ks = __ldcg(a.k_scales + (size_t)b * a.kv_heads + kv_head);
-                vs = __ldcg(a.v_scales + (size_t)b * a.kv_heads + kv_head);
-            }
-        };
-        if (n > 0) {
-            load(k, a.k_codes, number, 0);
-            load(v, a.v_codes, number, 0);
-            scales(number);
-        }
-        for (int j = 0; j < n; ++j) {
+        bool ok = true;
+        for (int j = 0; j < n && ok; ++j) {
             const int st = j & 1;
-            const uint32_t parity = ((j >> 1) & 1) ^ 1;
-            if (!ptx::warp_mbar_wait_suspend(bar(C::KE + st), parity, abort_flag)) break;
-            if (wv == 0) {
-                // a stage is free when its scores are complete, and those follow the weights of the step before: this slot's are used
-                if (lane < 8) {
-                    float lg, inv;
-                    kv8_value_scale(vs, lg, inv);
-                    if (number < 0) lg = -INFINITY, inv = 0.0f;
-                    ptx::sts128(base + C::META_OFF + (j % TC_META) * 128 + lane * 16, make_float4(__half2float(__ushort_as_half((uint16_t)ks)), lg, inv, 0.0f));
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+                if (!(ok = ptx::warp_mbar_wait_suspend(bar((kv ? C::VE : C::KE) + st), ((j >> 1) & 1) ^ 1, abort_flag))) break;
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const int at = 4 * j + 2 * kv + q, slot = at % C::SLOTS;
+                    if (!(ok = ptx::warp_mbar_wait_suspend(bar(C::RF + slot), (at / C::SLOTS) & 1, abort_flag))) break;
+                    convert(base + C::RAW_OFF + slot * C::RAW, base + (kv ? C::V_OFF : C::K_OFF) + st * C::TILE + q * 64 * 128);
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(bar(C::RE + slot));
                 }
+                if (!ok) break;
+                ptx::fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(bar(C::MF + j % TC_META));
+                if (lane == 0) ptx::mbar_arrive(bar((kv ? C::VF : C::KF) + st));
             }
-            store(k, base + C::K_OFF + st * C::TILE);
-            ptx::fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(bar(C::KF + st));
-            number = next;
-            load(k, a.k_codes, number, j + 1);
-            scales(number);
-            next = number_of(j + 2);
-            if (!ptx::warp_mbar_wait_suspend(bar(C::VE + st), parity, abort_flag)) break;
-            store(v, base + C::V_OFF + st * C::TILE);
-            ptx::fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(bar(C::VF + st));
-            load(v, a.v_codes, number, j + 1);
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
@@ -403,6 +369,70 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
             if (ptx::elect_one()) ptx::tc_commit(bar(C::FINAL));
             __syncwarp();
             ptx::mbar_wait(bar(C::FINAL), 0, abort_flag);    // nothing may still be executing when tensor memory is freed
+        } else if (warp == TC_WARP_FETCH) {
+            // ---- codes and scales.  Lane l holds block number and scales of positions 16 (l & 7) .. + 15 of step 4 i + (l >> 3), for these four
+            // steps and the next four.
+            struct Meta { int number; uint32_t ks, vs; };
+            const int32_t* table = a.table + (size_t)seq * a.table_width;
+            auto meta_of = [&](int j0) -> Meta {
+                Meta m = {-1, 0u, 0u};
+                const int j = j0 + (lane >> 3);
+                const long long pos = (long long)(t_lo + j) * TC_KEYS + 16 * (lane & 7);
+                if (j < n && pos < longest) {
+                    const int number = __ldcg(table + (pos >> a.log2_block));
+                    if ((unsigned)number < (unsigned)a.num_blocks) {
+                        const size_t at = (size_t)number * a.kv_heads + kv_head;
+                        m.number = number;
+                        m.ks = __ldcg(a.k_scales + at);
+                        m.vs = __ldcg(a.v_scales + at);
+                    } else {
+                        *a.status = W4A8_ERR_INDEX;          // positions of a block that does not exist count as not there
+                    }
+                }
+                return m;
+            };
+            const int per = min(64, 1 << a.log2_block), copies = 64 / per;       // positions per copy, copies per 64 positions
+            Meta cur = meta_of(0), nxt = meta_of(4);
+            bool ok = true;
+            for (int j = 0; j < n && ok; ++j) {
+                if (j && (j & 3) == 0) {
+                    cur = nxt;
+                    nxt = meta_of(j + 4);
+                }
+                for (int q = 0; q < 4; ++q) {
+                    const int at = 4 * j + q, slot = at % C::SLOTS, first = (j & 3) * 8 + (q & 1) * 4;
+                    if (!(ok = ptx::warp_mbar_wait_suspend(bar(C::RE + slot), ((at / C::SLOTS) & 1) ^ 1, abort_flag))) break;
+                    if (q == 0) {
+                        // The slot of the raw codes is free: the step that used it (one or two ago) is being converted, so the scores of the
+                        // second before that are complete, which follow the weights of the third: scales of five steps ago are no longer read.
+                        if ((lane >> 3) == (j & 3)) {
+                            float lg, inv;
+                            kv8_value_scale(cur.vs, lg, inv);
+                            if (cur.number < 0) lg = -INFINITY, inv = 0.0f;
+                            ptx::sts128(base + C::META_OFF + (j % TC_META) * 128 + (lane & 7) * 16,
+                                        make_float4(__half2float(__ushort_as_half((uint16_t)cur.ks)), lg, inv, 0.0f));
+                        }
+                        __syncwarp();
+                        if (lane == 0) ptx::mbar_arrive(bar(C::MF + j % TC_META));
+                    }
+                    // lane i < copies: the i-th copy
+                    const int number = __shfl_sync(0xFFFFFFFFu, cur.number, first + ((lane * per) >> 4 & 3));
+                    const bool mine = lane < copies && number >= 0;
+                    const uint32_t bytes = (uint32_t)(__popc(__ballot_sync(0xFFFFFFFFu, mine)) * per * D);
+                    if (lane == 0) ptx::mbar_arrive_expect_tx(bar(C::RF + slot), bytes);
+                    __syncwarp();
+                    if (mine) {
+                        const int inside = ((t_lo + j) * TC_KEYS + (q & 1) * 64 + lane * per) & ((1 << a.log2_block) - 1);
+                        const int8_t* src = (q < 2 ? a.k_codes : a.v_codes) + ((((size_t)number * a.kv_heads + kv_head) << a.log2_block) + inside) * D;
+                        ptx::bulk_g2s(base + C::RAW_OFF + slot * C::RAW + lane * per * D, src, per * D, bar(C::RF + slot));
+                    }
+                    __syncwarp();
+                }
+            }
+            if (!ok) {   // let copies already in flight land before shared memory is released
+                const uint64_t t0 = ptx::globaltimer_ns();
+                while (ptx::globaltimer_ns() - t0 < 200000ull) {}
+            }
         }
     }
     if (*abort_flag && lane == 0) atomicExch(a.status, (uint32_t)W4A8_ERR_TIMEOUT);
