@@ -32,14 +32,38 @@ struct TcCfg {
     static constexpr int RAW = 64 * D, SLOTS = D == 128 ? 4 : 8;  // codes of 64 positions; K, K, V, V of a step in turn
     static constexpr int RAW_OFF = 6 * TILE;
     static constexpr int BAR_OFF = RAW_OFF + SLOTS * RAW;
-    // barriers: K and V stages full and empty, scores and weights of a half, Q of a half, O of a half complete, scales, raw codes full and
+    // barriers: K and V stages full and empty, scores of a half and its weights in two parts, Q of a half, O of a half complete, scales, raw codes full and
     // empty, end
-    static constexpr int KF = 0, KE = 2, VF = 4, VE = 6, SF = 8, PF = 10, QF = 12, OF = 14, MF = 16, RF = MF + TC_META, RE = RF + SLOTS, FINAL = RE + SLOTS, NUM_BARS = FINAL + 1;
+    static constexpr int KF = 0, KE = 2, VF = 4, VE = 6, SF = 8, PF = 10, QF = 14, OF = 16, MF = 18, RF = MF + TC_META, RE = RF + SLOTS, FINAL = RE + SLOTS, NUM_BARS = FINAL + 1;
     static constexpr int META_OFF = (BAR_OFF + NUM_BARS * 8 + 15) & ~15;        // [TC_META][8] float4: key scale, log2 of the value scale, its reciprocal
     static constexpr int MISC_OFF = META_OFF + TC_META * 8 * 16;                // tensor-memory base, abort flag, longest limit
     static constexpr int SMEM = MISC_OFF + 16 + 1024;
     static constexpr uint32_t S_COL = 0, O_COL = 256;                            // tensor memory: scores 2 x 128 columns, sums 2 x 128
 };
+
+#ifndef TC_POLY
+#define TC_POLY 2
+#endif
+// 2^x and 2^y without the special-function unit: x = n + f with n the nearest integer (which lands in the low mantissa bits of x + 1.5 2^23), 2^f
+// on [-1/2, 1/2] by the polynomial of degree 4 with the smallest largest relative error, 2.6e-6 (Remez), n added to the exponent.
+// Below -126, 2^-126 or less; not-a-number stays no number that anything finite is made of.
+__device__ __forceinline__ float2 exp2_poly2(float x, float y) {
+    constexpr float C4 = 0.009570102207362652f, C3 = 0.05591785907745361f, C2 = 0.240247443318367f, C1 = 0.6931217908859253f, C0 = 0.9999992847442627f;
+    constexpr float MAGIC = 12582912.0f;
+    auto both = [](float v) { return ptx::pack2(__float_as_uint(v), __float_as_uint(v)); };
+    x = fmaxf(x, -126.0f);
+    y = fmaxf(y, -126.0f);
+    const uint64_t v = ptx::pack2(__float_as_uint(x), __float_as_uint(y));
+    const uint64_t t = ptx::add2(v, both(MAGIC));
+    const uint64_t n = ptx::add2(t, both(-MAGIC));
+    const uint64_t f = ptx::fma2(n, both(-1.0f), v);
+    uint64_t p = ptx::fma2(f, both(C4), both(C3));
+    p = ptx::fma2(p, f, both(C2));
+    p = ptx::fma2(p, f, both(C1));
+    p = ptx::fma2(p, f, both(C0));
+    const float2 r = ptx::unpack2(p), e = ptx::unpack2(t);
+    return make_float2(__uint_as_float(__float_as_uint(r.x) + (__float_as_uint(e.x) << 23)), __uint_as_float(__float_as_uint(r.y) + (__float_as_uint(e.y) << 23)));
+}
 
 template <int D>
 __global__ void __launch_bounds__(TC_THREADS, 1)
@@ -65,6 +89,7 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
                 ptx::mbar_init(bar(C::VE + i), 1);
                 ptx::mbar_init(bar(C::SF + i), 1);
                 ptx::mbar_init(bar(C::PF + i), 4);
+                ptx::mbar_init(bar(C::PF + 2 + i), 4);
                 ptx::mbar_init(bar(C::QF + i), 4);
                 ptx::mbar_init(bar(C::OF + i), 1);
             }
@@ -162,26 +187,37 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
                 for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(s_col + 32 * c, s[c]);
                 const uint32_t meta = base + C::META_OFF + (j % TC_META) * 128;
                 const int key0 = (t_lo + j) * TC_KEYS;
-                float off = ref == -INFINITY ? 0.0f : KV8_W_EXP - ref;
-                ptx::tmem_ld_wait();
-                float top = -INFINITY;
+                const float off = ref == -INFINITY ? 0.0f : KV8_W_EXP - ref;
+                uint64_t f2[8], add2[8];
 #pragma unroll
                 for (int b = 0; b < 8; ++b) {
-                    const uint4 m = ptx::lds128(meta + 16 * b);
-                    const float f = factor * __uint_as_float(m.x), add = __uint_as_float(m.y) + off;
+                    const uint2 m = ptx::lds64(meta + 16 * b);
+                    const uint32_t f = __float_as_uint(factor * __uint_as_float(m.x)), add = __float_as_uint(__uint_as_float(m.y) + off);
+                    f2[b] = ptx::pack2(f, f);
+                    add2[b] = ptx::pack2(add, add);
+                }
+                ptx::tmem_ld_wait();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        uint32_t& v = s[b >> 1][(b & 1) * 16 + i];
-                        v = __float_as_uint(fmaf(__uint_as_float(v), f, add));
-                    }
+                for (int i = 0; i < 128; i += 2) {
+                    uint32_t &x = s[i >> 5][i & 31], &y = s[i >> 5][(i & 31) + 1];
+                    const float2 z = ptx::unpack2(ptx::fma2(ptx::pack2(x, y), f2[i >> 4], add2[i >> 4]));
+                    x = __float_as_uint(z.x);
+                    y = __float_as_uint(z.y);
                 }
                 if (key0 + TC_KEYS > shortest) {
 #pragma unroll
                     for (int i = 0; i < 128; ++i)
                         if (key0 + i >= limit) s[i >> 5][i & 31] = __float_as_uint(-INFINITY);
                 }
+                float tops[4];
 #pragma unroll
-                for (int i = 0; i < 128; i += 2) top = fmaxf(top, fmaxf(__uint_as_float(s[i >> 5][i & 31]), __uint_as_float(s[i >> 5][(i + 1) & 31])));
+                for (int c = 0; c < 4; ++c) {
+                    tops[c] = __uint_as_float(s[c][0]);
+#pragma unroll
+                    for (int i = 1; i < 31; i += 2) tops[c] = fmaxf(tops[c], fmaxf(__uint_as_float(s[c][i]), __uint_as_float(s[c][i + 1])));
+                    tops[c] = fmaxf(tops[c], __uint_as_float(s[c][31]));
+                }
+                const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                 const bool past = top > (ref == -INFINITY ? -INFINITY : KV8_W_EXP + KV8_SLACK);
                 if (__any_sync(0xFFFFFFFFu, past)) {
                     // (a step's scores are complete only when the products of the step before are: O is at rest)
@@ -191,7 +227,7 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
                         f = ref == -INFINITY ? 0.0f : kv8_ex2(ref - now);
                         ref = now;
                         shift = KV8_W_EXP - ref - off;
-                        sum *= f;
+                        sum = now == INFINITY ? NAN : sum * f;                  // an infinite score: not a number from here on
                     }
                     __syncwarp();
 #pragma unroll
@@ -209,28 +245,34 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
                         }
                     }
                 }
+                // ---- the weights, handed over 64 positions at a time.  Some exponentials are taken by the polynomial, on the FMA pipe.
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     uint32_t p[32];
 #pragma unroll
                     for (int b = 0; b < 4; ++b) {
-                        float g0 = 0.0f, g1 = 0.0f;
+                        uint64_t g = 0;
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             const int at = (4 * c + b) * 16 + 2 * i;
-                            const float w0 = kv8_ex2(__uint_as_float(s[at >> 5][at & 31])), w1 = kv8_ex2(__uint_as_float(s[at >> 5][(at + 1) & 31]));
-                            g0 += w0;
-                            g1 += w1;
-                            p[b * 8 + i] = kv8_pack_half2(w0, w1);
+                            const float x = __uint_as_float(s[at >> 5][at & 31]), y = __uint_as_float(s[at >> 5][(at & 31) + 1]);
+                            float2 w;
+                            if (i % 8 < TC_POLY)
+                                w = exp2_poly2(x, y);
+                            else
+                                w = make_float2(kv8_ex2(x), kv8_ex2(y));
+                            g = ptx::add2(g, ptx::pack2(__float_as_uint(w.x), __float_as_uint(w.y)));
+                            p[b * 8 + i] = kv8_pack_half2(w.x, w.y);
                         }
-                        sum = fmaf(g0 + g1, __uint_as_float(ptx::lds32(meta + 16 * (4 * c + b) + 8)), sum);
+                        const float2 g2 = ptx::unpack2(g);
+                        sum = fmaf(g2.x + g2.y, __uint_as_float(ptx::lds32(meta + 16 * (4 * c + b) + 8)), sum);
                     }
                     ptx::tmem_st_32x32(s_col + 32 * c, p);
+                    ptx::tmem_st_wait();
+                    ptx::tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(bar(C::PF + 2 * h + c));
                 }
-                ptx::tmem_st_wait();
-                ptx::tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(bar(C::PF + h));
             }
             // ---- this thread's row of the result
             if (ok && n > 0) ok = ptx::warp_mbar_wait_suspend(bar(C::OF + h), 0, abort_flag);
@@ -344,19 +386,23 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
                 const int st = j & 1;
                 for (int h = 0; h < halves && ok; ++h) {
                     if (h == 0) ok = ptx::mbar_wait_suspend(bar(C::VF + st), (j >> 1) & 1, abort_flag);
-                    ok = ok && ptx::mbar_wait_suspend(bar(C::PF + h), j & 1, abort_flag);
-                    ok = __all_sync(0xFFFFFFFFu, ok);
-                    if (!ok) break;
-                    ptx::tc_fence_after_sync();
                     const uint64_t v0 = ptx::smem_desc_mn_sw128(base + C::V_OFF + st * C::TILE, C::PANEL);
-                    if (ptx::elect_one()) {
 #pragma unroll
-                        for (int i = 0; i < TC_KEYS / 16; ++i)
-                            ptx::mma_f16_ts(tm + C::O_COL + h * 128, tm + C::S_COL + h * 128 + 8 * i, v0 + (uint64_t)(i * 128), IDESC_O, j > 0 || i > 0);
-                        if (h == halves - 1) ptx::tc_commit(bar(C::VE + st));
-                        if (j == n - 1) ptx::tc_commit(bar(C::OF + h));
+                    for (int c = 0; c < 2; ++c) {
+                        ok = ok && ptx::mbar_wait_suspend(bar(C::PF + 2 * h + c), j & 1, abort_flag);
+                        ok = __all_sync(0xFFFFFFFFu, ok);
+                        if (!ok) break;
+                        ptx::tc_fence_after_sync();
+                        if (ptx::elect_one()) {
+#pragma unroll
+                            for (int i = 4 * c; i < 4 * c + 4; ++i)
+                                ptx::mma_f16_ts(tm + C::O_COL + h * 128, tm + C::S_COL + h * 128 + 8 * i, v0 + (uint64_t)(i * 128), IDESC_O, j > 0 || i > 0);
+                            if (c == 1 && h == halves - 1) ptx::tc_commit(bar(C::VE + st));
+                            if (c == 1 && j == n - 1) ptx::tc_commit(bar(C::OF + h));
+                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
+                    if (!ok) break;
                     if (j + 1 < n) {
                         if (h == 0) ok = ptx::mbar_wait_suspend(bar(C::KF + (st ^ 1)), ((j + 1) >> 1) & 1, abort_flag);
                         ok = __all_sync(0xFFFFFFFFu, ok);

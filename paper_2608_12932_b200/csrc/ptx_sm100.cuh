@@ -328,6 +328,11 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
 // acc += (v + b) * s for a pair v = (lo, hi), the accumulator updated in place
 __device__ __forceinline__ void add_fma2(uint64_t& acc, uint32_t lo, uint32_t hi, uint64_t b, uint64_t s) {
     asm("{\n\t.reg .b64 t;\n\t"
