@@ -229,6 +229,15 @@ def test_attention_rows(T, rep, heads, dim, block):
     c.check_attend(q, table, causal([keys], T))
 
 
+@pytest.mark.parametrize("B_,T,heads,rep,dim,block,keys", [(1, 1210, 8, 4, 128, 64, 1300), (3, 500, 8, 5, 64, 32, 640), (40, 40, 5, 7, 128, 128, 90)])
+def test_attention_of_more_tiles_than_are_resident(B_, T, heads, rep, dim, block, keys):
+    """Every kernel's later rounds: a CTA that walks several row tiles of different lengths, one of them without any key."""
+    _, c, table, q = attend_case(T + rep, B_, T, heads, rep, dim, block, keys)
+    limits = causal([keys - 13 * (b % 5) for b in range(B_)], T)
+    limits[B_ // 2, T // 2:T // 2 + 300] = 0
+    c.check_attend(q, table, limits)
+
+
 @pytest.mark.parametrize("T", [1, 8, 70])
 def test_attention_of_a_padded_batch(T):
     """Ragged sequences, some rows and one whole sequence that see nothing: those give zeros."""
