@@ -2,14 +2,17 @@
 // kv8_attention.cuh).
 //
 // kv8_attend_rows_kernel: one CTA per (sequence, key head, row tile, slice of the keys).  A row tile is 16 or 32 (token, head)
-// rows of one key head's group, so a group's heads share what is read of the cache.  Each of the four warps walks its own chunks of 16
-// positions with its own running sums: 16-byte asynchronous copies into a ring of its own (no block barrier in the loop),
-// mma.m16n8k16 with the rows on the 16-row side.  The order of the contraction index is free as long as both operands agree,
-// and so is the order of the output channels, so a lane takes 16 neighbouring codes of a key for the first product and 16
-// neighbouring channels of four values for the second, and converts them in registers: nothing is transposed through shared memory.
-// Bound by HBM as long as a chunk's 2 D B per position take longer than its products and conversions.
+// rows of one key head's group, so a group's heads share what is read of the cache.  Two pairs of warps walk chunks of 2 x 16 positions,
+// each pair with its own running sums: a warp fetches 16 positions' codes (16-byte asynchronous copies into a ring of its own), forms their
+// scores and weights, hands the weights to its partner through shared memory, and multiplies the values of all 32 positions for its half of the
+// channels.  So a warp keeps half a tile's sums: a warp that keeps all of them needs 255 registers at 32 rows, and two warps
+// per scheduler leave it idle most of the time (a draft block of 8 over 32749 positions: 39 us).
+// mma.m16n8k16 with the rows on the 16-row side.  The order of the contraction index is free as long as both operands
+// agree, and so is the order of the output channels, so a lane takes 16 neighbouring codes of a key for the first product and neighbouring
+// channels of four values for the second, and converts them in registers: nothing is transposed through shared memory.  The
+// weights come out of the first product as the second one's operand: a lane stores 16 bytes and its partner's lane loads them.
 //
-// kv8_combine_kernel: joins the slices' sums, one warp per row.
+// kv8_combine_kernel: joins the slices' sums.
 #include "kv8_attention.cuh"
 
 namespace w4a8 {
@@ -20,14 +23,21 @@ constexpr int AR_WARPS = 4, AR_CHUNK = 16;
 template <int D, int RB>
 struct ArCfg {
     static constexpr int ROWS = 16 * RB;
+    static constexpr int CTAS = RB == 1 ? 4 : 3;                          // per SM
     static constexpr int K_BYTES = AR_CHUNK * D;                          // codes of a chunk's keys; as many of its values
     static constexpr int STAGE = 2 * K_BYTES;
-    static constexpr int STAGES = 16384 / STAGE;                          // 16 KB in flight per warp
+    static constexpr int STAGES = 12288 / STAGE;                          // 12 KB per warp, one stage of it being worked on
     static constexpr int RING = AR_WARPS * STAGES * STAGE;
-    static constexpr int O_PITCH = D + 4;                                 // floats per row of the warps' sums at the end
-    static constexpr int JOIN = AR_WARPS * ROWS * O_PITCH * 4;
-    static constexpr int ML_OFF = RING > JOIN ? RING : JOIN;
+    static constexpr int O_PITCH = D + 4;                                 // floats per row of the pairs' sums at the end
+    static constexpr int JOIN = 2 * ROWS * O_PITCH * 4;
+    static constexpr int W_OFF = RING > JOIN ? RING : JOIN;               // weights on their way: [warp][turn & 1][RB][lane] 16 bytes
+    static constexpr int W_BYTES = RB * 512;
+    static constexpr int Q_OFF = W_OFF + AR_WARPS * 2 * W_BYTES;          // q as operand: [D / 16][RB][lane] 16 bytes (16 rows: in registers)
+    static constexpr int TOP_OFF = Q_OFF + (RB == 1 ? 0 : (D / 16) * RB * 512);           // rows' maxima where a reference moves: [warp][ROWS] float
+    static constexpr int FLAG_OFF = TOP_OFF + AR_WARPS * ROWS * 4;        // whether one does: [warp][turn & 1]
+    static constexpr int ML_OFF = FLAG_OFF + AR_WARPS * 8;                // at the end: references and sums of each warp's positions
     static constexpr int SMEM = ML_OFF + AR_WARPS * ROWS * 8;
+    static_assert(CTAS * (SMEM + 1024) <= 228 * 1024, "shared memory");
 };
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
@@ -52,26 +62,30 @@ __device__ __forceinline__ uint32_t chunk_at(int r, int p) {
 }
 
 template <int D, int RB>
-__global__ void __launch_bounds__(AR_WARPS * 32)
+__global__ void __launch_bounds__(AR_WARPS * 32, (ArCfg<D, RB>::CTAS))
 kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     using C = ArCfg<D, RB>;
     constexpr int KS = D / 16;                               // k steps of the first product = words of codes per lane and key
+    constexpr int NB = D / 16;                               // 8-channel blocks of this warp's half of the second product
     extern __shared__ __align__(128) uint8_t smem_raw[];
     const uint32_t smem = ptx::smem_u32(smem_raw);
     ptx::pdl_launch_dependents();
     const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31, g = lane >> 2, t = lane & 3;
+    const int pair = warp >> 1, side = warp & 1;
     const int tile = blockIdx.x / a.slices, slice = blockIdx.x - tile * a.slices, kv_head = blockIdx.z % a.kv_heads, seq = blockIdx.z / a.kv_heads;
     const int rows = a.T * a.rep, row0 = tile * C::ROWS;
     ptx::pdl_wait();
 
-    // ---- this lane's rows: limits, q as fp16, and the factor that undoes its power of two
+    // ---- this lane's rows: limits, q as fp16, and the factor that undoes its power of two.  With 32 rows q goes to shared memory, each warp
+    // a part.
     int limit[RB][2];
     float factor[RB][2];
-    uint32_t qf[RB][KS][4];
+    uint32_t qf[RB == 1 ? KS : 1][4];
     int longest = 0, shortest = 0x7FFFFFFF;
     const int capacity = (int)min((long long)a.table_width << a.log2_block, 0x7FFFFFF0ll);
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
+        uint32_t q2[KS][4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int r = row0 + rb * 16 + h * 8 + g;
@@ -104,198 +118,281 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
             factor[rb][h] = a.scale_log2 * kv8_pow2(-e);
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
-                qf[rb][i][h] = kv8_pack_half2(__uint_as_float(w[2 * i] << 16) * up, __uint_as_float(w[2 * i] & 0xFFFF0000u) * up);
-                qf[rb][i][2 + h] = kv8_pack_half2(__uint_as_float(w[2 * i + 1] << 16) * up, __uint_as_float(w[2 * i + 1] & 0xFFFF0000u) * up);
+                q2[i][h] = kv8_pack_half2(__uint_as_float(w[2 * i] << 16) * up, __uint_as_float(w[2 * i] & 0xFFFF0000u) * up);
+                q2[i][2 + h] = kv8_pack_half2(__uint_as_float(w[2 * i + 1] << 16) * up, __uint_as_float(w[2 * i + 1] & 0xFFFF0000u) * up);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            if (RB == 1) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) qf[i % (RB == 1 ? KS : 1)][k] = q2[i][k];
+            } else if (i % AR_WARPS == warp) {
+                ptx::sts128u(smem + C::Q_OFF + ((i * RB + rb) * 32 + lane) * 16, q2[i][0], q2[i][1], q2[i][2], q2[i][3]);
             }
         }
     }
     longest = __reduce_max_sync(0xFFFFFFFFu, longest);
     shortest = __reduce_min_sync(0xFFFFFFFFu, shortest);
+    if (lane < 2) asm volatile("st.shared.u32 [%0], %1;" ::"r"(smem + C::FLAG_OFF + warp * 8 + lane * 4), "r"(0u) : "memory");
 
-    // ---- this CTA's chunks of 16 positions, dealt to the warps in turn
+    // ---- this CTA's chunks of 16 positions, dealt in twos to the pairs in turn, one of the two to each warp
     const int chunks = (int)(((long long)longest + AR_CHUNK - 1) / AR_CHUNK);
     const int c_lo = (int)((long long)slice * chunks / a.slices), c_hi = (int)((long long)(slice + 1) * chunks / a.slices);
-    const int mine = (c_hi - c_lo - warp + AR_WARPS - 1) / AR_WARPS;
+    const int turns = (c_hi - c_lo - 2 * pair + 3) / 4;      // of the pair
+    const int first = c_lo + warp;                           // this warp's chunk of turn i: first + 4 i (none where that is c_hi or more)
     const int chunk_shift = a.log2_block - 4;                // chunks per block, as a shift
     const int32_t* table = a.table + (size_t)seq * a.table_width;
-    // lane j holds block number and scales of chunk 32 i + j of this warp, for the current 32 chunks and the next
-    struct Meta { int number; uint32_t ks, vs; };
+    // lane j holds block number and scales of this warp's chunk of turn 32 i + j, for the current 32 turns and the next
+    struct Meta { int number; uint32_t scales; };            // scales: key's, value's
     auto meta_of = [&](int base) -> Meta {
-        Meta m = {-1, 0u, 0u};
-        const int i = base + lane;
-        if (i < mine) {
-            const int number = __ldcg(table + ((c_lo + warp + AR_WARPS * i) >> chunk_shift));
+        Meta m = {-1, 0u};
+        const int c = first + 4 * (base + lane);
+        if (base + lane < turns && c < c_hi) {
+            const int number = __ldcg(table + (c >> chunk_shift));
             if ((unsigned)number < (unsigned)a.num_blocks) {
                 const size_t at = (size_t)number * a.kv_heads + kv_head;
                 m.number = number;
-                m.ks = __ldcg(a.k_scales + at);
-                m.vs = __ldcg(a.v_scales + at);
+                m.scales = (uint32_t)__ldcg(a.k_scales + at) | (uint32_t)__ldcg(a.v_scales + at) << 16;
             } else {
                 *a.status = W4A8_ERR_INDEX;                  // positions of a block that does not exist count as not there
             }
         }
         return m;
     };
-    Meta cur = meta_of(0), nxt = meta_of(32);
+    Meta cur = meta_of(0), nxt = {-1, 0u};
+    if (turns > 32) nxt = meta_of(32);
     int base = 0;
-    const uint32_t ring = smem + warp * (C::STAGES * C::STAGE);
+    const uint32_t ring = smem + warp * (C::STAGES * C::STAGE), other_ring = smem + (warp ^ 1) * (C::STAGES * C::STAGE);
+    int slot_in = 0;
     auto issue = [&](int i) {
-        if (i < mine) {
+        if (i < turns) {
             const int number = __shfl_sync(0xFFFFFFFFu, i - base < 32 ? cur.number : nxt.number, i & 31);
             if (number >= 0) {
-                const int c = c_lo + warp + AR_WARPS * i;
-                const int slot = (c & ((1 << chunk_shift) - 1)) * AR_CHUNK;
-                const size_t at = ((((size_t)number * a.kv_heads + kv_head) << a.log2_block) + slot) * D;
-                const uint32_t dst = ring + (i % C::STAGES) * C::STAGE;
+                const int inside = ((first + 4 * i) & ((1 << chunk_shift) - 1)) * AR_CHUNK;
+                const size_t at = ((((size_t)number * a.kv_heads + kv_head) << a.log2_block) + inside) * D + lane * 16;
+                const int8_t *k = a.k_codes + at, *v = a.v_codes + at;
+                const uint32_t dst = ring + slot_in * C::STAGE;
 #pragma unroll
                 for (int j = 0; j < C::K_BYTES / 512; ++j) {
                     const int idx = j * 32 + lane, r = idx / (D / 16), p = idx % (D / 16);
-                    cp_async16(dst + chunk_at<D>(r, p), a.k_codes + at + idx * 16);
-                    cp_async16(dst + C::K_BYTES + chunk_at<D>(r, p), a.v_codes + at + idx * 16);
+                    cp_async16(dst + chunk_at<D>(r, p), k + j * 512);
+                    cp_async16(dst + C::K_BYTES + chunk_at<D>(r, p), v + j * 512);
                 }
             }
         }
+        slot_in = slot_in + 1 == C::STAGES ? 0 : slot_in + 1;
         cp_async_commit();
     };
 #pragma unroll
     for (int i = 0; i < C::STAGES - 1; ++i) issue(i);
+    __syncthreads();                                         // q and flags are there
 
-    float o[RB][D / 8][4];
+    float o[RB][NB][4];
     float ref[RB][2], sum[RB][2];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
-        for (int j = 0; j < D / 8; ++j) o[rb][j][0] = o[rb][j][1] = o[rb][j][2] = o[rb][j][3] = 0.0f;
+        for (int j = 0; j < NB; ++j) o[rb][j][0] = o[rb][j][1] = o[rb][j][2] = o[rb][j][3] = 0.0f;
         ref[rb][0] = ref[rb][1] = -INFINITY;
         sum[rb][0] = sum[rb][1] = 0.0f;
     }
-    for (int i = 0; i < mine; ++i) {
+    const uint32_t w_out = smem + C::W_OFF + warp * (2 * C::W_BYTES) + lane * 16, w_in = smem + C::W_OFF + (warp ^ 1) * (2 * C::W_BYTES) + lane * 16;
+    const uint32_t flag_out = smem + C::FLAG_OFF + warp * 8, flag_in = smem + C::FLAG_OFF + (warp ^ 1) * 8;
+    int slot = 0;
+    for (int i = 0; i < turns; ++i) {
         if (i == base + 32) {
             base += 32;
             cur = nxt;
-            nxt = meta_of(base + 32);
+            if (turns > base + 32) nxt = meta_of(base + 32);
         }
         cp_async_wait<C::STAGES - 2>();
         __syncwarp();
-        issue(i + C::STAGES - 1);
         const int number = __shfl_sync(0xFFFFFFFFu, cur.number, i & 31);
-        const uint32_t ks_bits = __shfl_sync(0xFFFFFFFFu, cur.ks, i & 31), vs_bits = __shfl_sync(0xFFFFFFFFu, cur.vs, i & 31);
-        if (number < 0) continue;
-        const int key0 = (c_lo + warp + AR_WARPS * i) * AR_CHUNK;
-        const uint32_t kst = ring + (i % C::STAGES) * C::STAGE, vst = kst + C::K_BYTES;
-        // ---- scores of 16 positions: columns 8 n + 2 t, + 1
+        const uint32_t scales = __shfl_sync(0xFFFFFFFFu, cur.scales, i & 31);
+        const int key0 = (first + 4 * i) * AR_CHUNK;
+        const uint32_t kst = ring + slot * C::STAGE;
+        // ---- scores of this warp's 16 positions: columns 8 n + 2 t, + 1
         float s[RB][2][4];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
             for (int n = 0; n < 2; ++n) s[rb][n][0] = s[rb][n][1] = s[rb][n][2] = s[rb][n][3] = 0.0f;
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
+        for (int i4 = 0; i4 < D / 64; ++i4) {
+            const uint4 x0 = ptx::lds128(kst + chunk_at<D>(g, t + 4 * i4)), x1 = ptx::lds128(kst + chunk_at<D>(8 + g, t + 4 * i4));
+            const uint32_t w[2][4] = {{x0.x, x0.y, x0.z, x0.w}, {x1.x, x1.y, x1.z, x1.w}};
 #pragma unroll
-            for (int i4 = 0; i4 < D / 64; ++i4) {
-                const uint4 x = ptx::lds128(kst + chunk_at<D>(8 * n + g, t + 4 * i4));
-                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+            for (int j = 0; j < 4; ++j) {
+                uint32_t q[RB][4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t u = w[j] ^ 0x80808080u;
+                for (int rb = 0; rb < RB; ++rb) {
+                    if (RB == 1) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) q[rb][k] = qf[(4 * i4 + j) % (RB == 1 ? KS : 1)][k];
+                    } else {
+                        const uint4 y = ptx::lds128(smem + C::Q_OFF + (((4 * i4 + j) * RB + rb) * 32 + lane) * 16);
+                        q[rb][0] = y.x, q[rb][1] = y.y, q[rb][2] = y.z, q[rb][3] = y.w;
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    const uint32_t u = w[n][j] ^ 0x80808080u;
                     const uint32_t b0 = kv8_half2(u, 0x4140), b1 = kv8_half2(u, 0x4342);
 #pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) mma_f16(s[rb][n], qf[rb][4 * i4 + j], b0, b1);
+                    for (int rb = 0; rb < RB; ++rb) mma_f16(s[rb][n], q[rb], b0, b1);
                 }
             }
         }
         float lg, inv;
-        kv8_value_scale(vs_bits, lg, inv);
-        const float ks = __half2float(__ushort_as_half((uint16_t)ks_bits));
-        // ---- weights: x = score in base 2 + log2 of the value scale
+        kv8_value_scale(scales >> 16, lg, inv);
+        const float ks = __half2float(__ushort_as_half((uint16_t)scales));
+        // ---- weights at the references as they are: 2^x, x the score in base 2 + log2 of the value scale - reference + 7
+        const bool none = number < 0, part = none || key0 + AR_CHUNK > shortest;
         bool past = false;
+        uint32_t wf[RB][4];
+        float more[RB][2];
+        auto weigh = [&]() {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float all = 0.0f;
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        const float w0 = kv8_ex2(s[rb][n][2 * h]), w1 = kv8_ex2(s[rb][n][2 * h + 1]);
+                        all += w0 + w1;
+                        wf[rb][2 * n + h] = kv8_pack_half2(w0, w1);
+                    }
+                    more[rb][h] = all;
+                }
+                ptx::sts128u(w_out + (i & 1) * C::W_BYTES + rb * 512, wf[rb][0], wf[rb][1], wf[rb][2], wf[rb][3]);
+            }
+        };
+        float off[RB][2];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const float f = factor[rb][h] * ks, most = ref[rb][h] + KV8_SLACK;
+                off[rb][h] = ref[rb][h] == -INFINITY ? 0.0f : KV8_W_EXP - ref[rb][h];
+                const float f = factor[rb][h] * ks, add = lg + off[rb][h];
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        float& x = s[rb][n][2 * h + j];
-                        x = fmaf(x, f, lg);
-                        if (key0 + AR_CHUNK > shortest && key0 + 8 * n + 2 * t + j >= limit[rb][h]) x = -INFINITY;
-                        past |= x > most;
-                    }
+                    for (int j = 0; j < 2; ++j) s[rb][n][2 * h + j] = fmaf(s[rb][n][2 * h + j], f, add);
                 }
             }
         }
-        if (__any_sync(0xFFFFFFFFu, past)) {
-            // some weight would pass the range that fp16 leaves for it: the references move to the rows' maxima
+        if (part) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (none || key0 + 8 * (e >> 2) + 2 * t + (e & 1) >= limit[rb][(e >> 1) & 1]) s[rb][e >> 2][e & 3] = -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float top = fmaxf(fmaxf(s[rb][0][2 * h], s[rb][0][2 * h + 1]), fmaxf(s[rb][1][2 * h], s[rb][1][2 * h + 1]));
+                past |= top > (ref[rb][h] == -INFINITY ? -INFINITY : KV8_W_EXP + KV8_SLACK);
+            }
+        }
+        past = __any_sync(0xFFFFFFFFu, past);
+        weigh();
+        if (past) {
+            // some weight is past the range that fp16 leaves for it: the rows' maxima, for both warps of the pair
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     float top = fmaxf(fmaxf(s[rb][0][2 * h], s[rb][0][2 * h + 1]), fmaxf(s[rb][1][2 * h], s[rb][1][2 * h + 1]));
                     top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-                    top = fmaxf(top, ref[rb][h]);
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2)) - off[rb][h];
+                    if (t == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(smem + C::TOP_OFF + (warp * C::ROWS + rb * 16 + h * 8 + g) * 4), "f"(top) : "memory");
+                }
+            }
+            if (lane == 0) asm volatile("st.shared.u32 [%0], 1;" ::"r"(flag_out + (i & 1) * 4) : "memory");
+        }
+        ptx::named_bar_sync(1 + pair, 64);                   // the pair's weights are there, and both warps' values; it is done with the turn before
+        issue(i + C::STAGES - 1);
+        const bool theirs = ptx::lds32(flag_in + (i & 1) * 4) != 0u;
+        if (past || theirs) {
+            // the references move to the larger of what they are and the maxima, and the weights of the turn are made anew
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float top = ref[rb][h];
+                    const int r = rb * 16 + h * 8 + g;
+                    if (past) top = fmaxf(top, __uint_as_float(ptx::lds32(smem + C::TOP_OFF + (warp * C::ROWS + r) * 4)));
+                    if (theirs) top = fmaxf(top, __uint_as_float(ptx::lds32(smem + C::TOP_OFF + ((warp ^ 1) * C::ROWS + r) * 4)));
                     const float f = ref[rb][h] == -INFINITY ? 0.0f : kv8_ex2(ref[rb][h] - top);
                     ref[rb][h] = top;
-                    sum[rb][h] *= f;
+                    sum[rb][h] = top == INFINITY ? NAN : sum[rb][h] * f;        // an infinite score: not a number from here on
+                    const float shift = (top == -INFINITY ? 0.0f : KV8_W_EXP - top) - off[rb][h];
 #pragma unroll
-                    for (int j = 0; j < D / 8; ++j) {
-                        o[rb][j][2 * h] *= f;
-                        o[rb][j][2 * h + 1] *= f;
-                    }
+                    for (int n = 0; n < 2; ++n) s[rb][n][2 * h] += shift, s[rb][n][2 * h + 1] += shift;
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) o[rb][j][2 * h] *= f, o[rb][j][2 * h + 1] *= f;
+                }
+            }
+            weigh();
+            ptx::named_bar_sync(1 + pair, 64);
+            if (lane == 0) asm volatile("st.shared.u32 [%0], 0;" ::"r"(flag_out + (i & 1) * 4) : "memory");
+        }
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) sum[rb][h] = fmaf(more[rb][h], inv, sum[rb][h]);
+        // ---- o += weights x values, this warp's half of the channels: positions 2 t, 2 t + 1, 2 t + 8, 2 t + 9 of either warp's 16, channels
+        // NB g + j of the half
+#pragma unroll
+        for (int turn = 0; turn < 2; ++turn) {
+            const uint32_t vst = (turn ? other_ring : ring) + slot * C::STAGE + C::K_BYTES;
+            if (turn) {
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) {
+                    const uint4 x = ptx::lds128(w_in + (i & 1) * C::W_BYTES + rb * 512);
+                    wf[rb][0] = x.x, wf[rb][1] = x.y, wf[rb][2] = x.z, wf[rb][3] = x.w;
+                }
+            }
+            uint32_t v[4][NB / 4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int r = 2 * t + (k & 1) + 8 * (k >> 1);
+                if (D == 128) {
+                    const uint2 x = ptx::lds64(vst + chunk_at<D>(r, 4 * side + (g >> 1)) + 8 * (g & 1));
+                    v[k][0] = x.x, v[k][NB / 4 - 1] = x.y;
+                } else {
+                    v[k][0] = ptx::lds32(vst + chunk_at<D>(r, 2 * side + (g >> 2)) + 4 * (g & 3));
+                }
+            }
+#pragma unroll
+            for (int i4 = 0; i4 < NB / 4; ++i4) {
+                uint32_t p[2][2];                            // positions (0, 1) and (2, 3): channels 0 1 and 2 3 of this word, position by position
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const uint32_t x = v[2 * k][i4] ^ 0x80808080u, y = v[2 * k + 1][i4] ^ 0x80808080u;
+                    p[k][0] = __byte_perm(x, y, 0x5140);
+                    p[k][1] = __byte_perm(x, y, 0x7362);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t sel = j & 1 ? 0x4342 : 0x4140;
+                    const uint32_t b0 = kv8_half2(p[0][j >> 1], sel), b1 = kv8_half2(p[1][j >> 1], sel);
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) mma_f16(o[rb][4 * i4 + j], wf[rb], b0, b1);
                 }
             }
         }
-        uint32_t wf[RB][4];
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float off = ref[rb][h] == -INFINITY ? 0.0f : KV8_W_EXP - ref[rb][h];       // (no position seen yet: weights 0)
-#pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    const float w0 = kv8_ex2(s[rb][n][2 * h] + off), w1 = kv8_ex2(s[rb][n][2 * h + 1] + off);
-                    sum[rb][h] = fmaf(w0 + w1, inv, sum[rb][h]);
-                    wf[rb][2 * n + h] = kv8_pack_half2(w0, w1);
-                }
-            }
-        }
-        // ---- o += weights x values: this lane's positions 2 t, 2 t + 1, 2 t + 8, 2 t + 9, channels (D / 8) g + j
-        uint32_t v[4][D / 32];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int r = 2 * t + (k & 1) + 8 * (k >> 1);
-            if (D == 128) {
-                const uint4 x = ptx::lds128(vst + chunk_at<D>(r, g));
-                v[k][0] = x.x, v[k][1] = x.y, v[k][D / 32 - 2] = x.z, v[k][D / 32 - 1] = x.w;
-            } else {
-                const uint2 x = ptx::lds64(vst + chunk_at<D>(r, g >> 1) + 8 * (g & 1));
-                v[k][0] = x.x, v[k][1] = x.y;
-            }
-        }
-#pragma unroll
-        for (int i4 = 0; i4 < D / 32; ++i4) {
-            uint32_t p[2][2];                                // positions (0, 1) and (2, 3): channels 0 1 and 2 3 of this word, position by position
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const uint32_t x = v[2 * k][i4] ^ 0x80808080u, y = v[2 * k + 1][i4] ^ 0x80808080u;
-                p[k][0] = __byte_perm(x, y, 0x5140);
-                p[k][1] = __byte_perm(x, y, 0x7362);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t sel = j & 1 ? 0x4342 : 0x4140;
-                const uint32_t b0 = kv8_half2(p[0][j >> 1], sel), b1 = kv8_half2(p[1][j >> 1], sel);
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) mma_f16(o[rb][4 * i4 + j], wf[rb], b0, b1);
-            }
-        }
+        slot = slot + 1 == C::STAGES ? 0 : slot + 1;
     }
     cp_async_wait<0>();
-    __syncthreads();                                         // the rings are free: they take the warps' sums
+    __syncthreads();                                         // the rings are free: they take the pairs' sums
 
-    // ---- the four warps' sums, joined
+    // ---- the two pairs' sums, joined
     float* join = reinterpret_cast<float*>(smem_raw);
     float2* ml = reinterpret_cast<float2*>(smem_raw + C::ML_OFF);
 #pragma unroll
@@ -307,13 +404,13 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
             l += __shfl_xor_sync(0xFFFFFFFFu, l, 1);
             l += __shfl_xor_sync(0xFFFFFFFFu, l, 2);
             if (t == 0) ml[warp * C::ROWS + r] = make_float2(ref[rb][h], l);
-            // columns 2 t and 2 t + 1 of product j are channels (D / 8) (2 t) + j and (D / 8) (2 t + 1) + j
-            float* dst = join + (warp * C::ROWS + r) * C::O_PITCH + (D / 8) * 2 * t;
+            // columns 2 t and 2 t + 1 of product j are channels NB 2 t + j and NB (2 t + 1) + j of the half
+            float* dst = join + (pair * C::ROWS + r) * C::O_PITCH + side * (D / 2) + NB * 2 * t;
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
 #pragma unroll
-                for (int j = 0; j < D / 8; j += 4)
-                    *reinterpret_cast<float4*>(dst + c * (D / 8) + j) = make_float4(o[rb][j][2 * h + c], o[rb][j + 1][2 * h + c], o[rb][j + 2][2 * h + c], o[rb][j + 3][2 * h + c]);
+                for (int j = 0; j < NB; j += 4)
+                    *reinterpret_cast<float4*>(dst + c * NB + j) = make_float4(o[rb][j][2 * h + c], o[rb][j + 1][2 * h + c], o[rb][j + 2][2 * h + c], o[rb][j + 3][2 * h + c]);
             }
         }
     }
@@ -324,16 +421,16 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
         if (row >= rows) break;
         float m = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < AR_WARPS; ++w) m = fmaxf(m, ml[w * C::ROWS + r].x);
+        for (int w = 0; w < 2; ++w) m = fmaxf(m, ml[2 * w * C::ROWS + r].x);
         float l = 0.0f;
         float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-        for (int w = 0; w < AR_WARPS; ++w) {
-            const float2 one = ml[w * C::ROWS + r];
+        for (int w = 0; w < 2; ++w) {
+            const float2 one = ml[2 * w * C::ROWS + r], two = ml[(2 * w + 1) * C::ROWS + r];
             // (a row without a reference has no weights, or is not a number in all of them)
             const float f = one.x == -INFINITY ? 1.0f : kv8_ex2(one.x - m);
             const float4 y = *reinterpret_cast<const float4*>(join + (w * C::ROWS + r) * C::O_PITCH + d);
-            l = fmaf(f, one.y, l);
+            l = fmaf(f, one.y + two.y, l);
             x.x = fmaf(f, y.x, x.x);
             x.y = fmaf(f, y.y, x.y);
             x.z = fmaf(f, y.z, x.z);
@@ -351,16 +448,19 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     }
 }
 
-// One warp per (token, head) row: the slices' sums, each weighted by how far its reference is below the largest.
-template <int D>
+// W warps per (token, head) row, each with its share of the slices: sums weighted by how far their reference is below the largest.  With four
+// warps per row one decode token's 32 slices take one round of loads (one warp per row took most of 6 us); up to eight slices, and so with many
+// rows, one warp has them under way at once (four: 200 rows of 28 heads 38.7 instead of 29 us altogether).
+template <int D, int W>
 __global__ void __launch_bounds__(128)
-kv8_combine_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, uint16_t* __restrict__ out, long long total_rows,
-                   int T, int q_heads, int kv_heads, int rep, int tiles, int slices, int tile_rows) {
+kv8_combine_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, uint16_t* __restrict__ out, long long total_rows, int T,
+                   int q_heads, int kv_heads, int rep, int tiles, int slices, int tile_rows) {
     constexpr int V = D / 32;
+    __shared__ float sums[W == 1 ? 1 : W][W == 1 ? 1 : D];
+    __shared__ float2 refs[W];
     ptx::pdl_launch_dependents();
-    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
-    ptx::pdl_wait();
+    const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long long row = W == 1 ? (long long)blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
     if (row >= total_rows) return;
     const int head = (int)(row % q_heads);
     const long long at = row / q_heads;                      // seq T + token
@@ -368,38 +468,76 @@ kv8_combine_kernel(const float* __restrict__ part_o, const float2* __restrict__ 
     const long long r = (long long)token * rep + head - kv_head * rep;
     const size_t unit = (((size_t)(at / T) * kv_heads + kv_head) * tiles + (size_t)(r / tile_rows)) * slices;
     const size_t first = unit * tile_rows + (size_t)(r % tile_rows);
-    float m = -INFINITY;
-    for (int z = lane; z < slices; z += 32) m = fmaxf(m, __ldcg(&part_ml[first + (size_t)z * tile_rows]).x);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-    float l = 0.0f, x[V];
+    ptx::pdl_wait();
+    float m = -INFINITY, l = 0.0f, x[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) x[i] = 0.0f;
-#pragma unroll 4
-    for (int z = 0; z < slices; ++z) {
-        const size_t p = first + (size_t)z * tile_rows;
-        const float2 one = __ldcg(&part_ml[p]);
-        const float f = one.x == -INFINITY ? 1.0f : kv8_ex2(one.x - m);
-        l = fmaf(f, one.y, l);
-        const float* src = part_o + p * D + lane * V;
-        if (V == 4) {
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(src));
-            x[0] = fmaf(f, y.x, x[0]);
-            x[1] = fmaf(f, y.y, x[1]);
-            x[V - 2] = fmaf(f, y.z, x[V - 2]);
-            x[V - 1] = fmaf(f, y.w, x[V - 1]);
-        } else {
-            const float2 y = __ldcg(reinterpret_cast<const float2*>(src));
-            x[0] = fmaf(f, y.x, x[0]);
-            x[1] = fmaf(f, y.y, x[1]);
+    // eight slices at a time, all loads ahead of the first use
+    constexpr int U = 8;
+    for (int z0 = warp; z0 < slices; z0 += W * U) {
+        float2 one[U];
+        float y[U][V];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int z = z0 + W * u;
+            one[u] = make_float2(-INFINITY, 0.0f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) y[u][i] = 0.0f;
+            if (z < slices) {
+                const size_t p = first + (size_t)z * tile_rows;
+                one[u] = __ldcg(&part_ml[p]);
+                const float2* src = reinterpret_cast<const float2*>(part_o + p * D + lane * V);
+#pragma unroll
+                for (int i = 0; i < V; i += 2) {
+                    const float2 v = __ldcg(src + i / 2);
+                    y[u][i] = v.x;
+                    y[u][i + 1] = v.y;
+                }
+            }
+        }
+        float top = m;
+#pragma unroll
+        for (int u = 0; u < U; ++u) top = fmaxf(top, one[u].x);
+        const float back = m == -INFINITY ? 1.0f : kv8_ex2(m - top);
+        m = top;
+        l *= back;
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] *= back;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            // (a slice without a reference has no weights, or is not a number in all of them)
+            const float f = one[u].x == -INFINITY ? 1.0f : kv8_ex2(one[u].x - m);
+            l = fmaf(f, one[u].y, l);
+#pragma unroll
+            for (int i = 0; i < V; ++i) x[i] = fmaf(f, y[u][i], x[i]);
         }
     }
-    const float inv = l == 0.0f ? 0.0f : __fdividef(1.0f, l);
-    uint32_t* dst = reinterpret_cast<uint32_t*>(out + row * D) + lane * (V / 2);
-    if (V == 4)
-        *reinterpret_cast<uint2*>(dst) = make_uint2(ptx::pack_bf16x2(x[0] * inv, x[1] * inv), ptx::pack_bf16x2(x[V - 2] * inv, x[V - 1] * inv));
-    else
-        *dst = ptx::pack_bf16x2(x[0] * inv, x[1] * inv);
+    if constexpr (W == 1) {
+        const float inv = l == 0.0f ? 0.0f : __fdividef(1.0f, l);
+        uint32_t* dst = reinterpret_cast<uint32_t*>(out + row * D) + lane * (V / 2);
+#pragma unroll
+        for (int i = 0; i < V; i += 2) dst[i / 2] = ptx::pack_bf16x2(x[i] * inv, x[i + 1] * inv);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) sums[warp][lane * V + i] = x[i];
+        if (lane == 0) refs[warp] = make_float2(m, l);
+        __syncthreads();
+        if (threadIdx.x >= D / 2) return;
+        m = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < W; ++w) m = fmaxf(m, refs[w].x);
+        float2 total = make_float2(0.0f, 0.0f);
+        l = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float f = refs[w].x == -INFINITY ? 1.0f : kv8_ex2(refs[w].x - m);
+            l = fmaf(f, refs[w].y, l);
+            total.x = fmaf(f, sums[w][2 * threadIdx.x], total.x);
+            total.y = fmaf(f, sums[w][2 * threadIdx.x + 1], total.y);
+        }
+        const float inv = l == 0.0f ? 0.0f : __fdividef(1.0f, l);
+        reinterpret_cast<uint32_t*>(out + row * D)[threadIdx.x] = ptx::pack_bf16x2(total.x * inv, total.y * inv);
+    }
 }
 
 template <int D, int RB>
@@ -430,9 +568,10 @@ cudaError_t launch_rows(const AttendArgs& a, int B, cudaStream_t stream) {
 
 template <int D>
 cudaError_t launch_combine(const AttendArgs& a, int B, int tile_rows, cudaStream_t stream) {
-    const long long total = (long long)B * a.T * a.q_heads;
+    const long long total = (long long)B * a.T * a.q_heads;              // few: there are slices only where tiles are
+    const bool one = a.slices <= 8;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((total + 3) / 4), 1, 1);
+    cfg.gridDim = dim3((unsigned)(one ? (total + 3) / 4 : total), 1, 1);
     cfg.blockDim = dim3(128, 1, 1);
     cfg.stream = stream;
     cudaLaunchAttribute attr;
@@ -440,14 +579,14 @@ cudaError_t launch_combine(const AttendArgs& a, int B, int tile_rows, cudaStream
     attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kv8_combine_kernel<D>, (const float*)a.part_o, (const float2*)a.part_ml, a.out, total, a.T, a.q_heads,
-                              a.kv_heads, a.rep, a.tiles, a.slices, tile_rows);
+    return cudaLaunchKernelEx(&cfg, one ? kv8_combine_kernel<D, 1> : kv8_combine_kernel<D, 4>, (const float*)a.part_o, (const float2*)a.part_ml, a.out,
+                              total, a.T, a.q_heads, a.kv_heads, a.rep, a.tiles, a.slices, tile_rows);
 }
 
 }  // namespace
 
-// Row tiles of 16 with three CTAs per SM, of 32 with two, of 256 with one: what is resident at once.
-static int ctas_per_sm(int rows) { return rows == 16 ? 3 : (rows == 32 ? 2 : 1); }
+// Row tiles of 16 with four CTAs per SM, of 32 with three, of 256 with one: what is resident at once.
+static int ctas_per_sm(int rows) { return rows == 16 ? ArCfg<128, 1>::CTAS : (rows == 32 ? ArCfg<128, 2>::CTAS : 1); }
 
 Kv8Plan kv8_plan(int B, int T, int q_heads, int kv_heads, long long max_keys, int sms) {
     Kv8Plan p;
