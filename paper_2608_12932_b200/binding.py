@@ -319,40 +319,55 @@ def w4a8_streaming_mask(views, frames, tokens_per_frame, device="cuda", stream=N
     return mask
 
 
-def _here(*tensors):
-    """The tensors (None among them allowed) must lie on the current device, where the call enqueues its work."""
-    index = torch._C._cuda_getDevice()
-    for t in tensors:
-        if t is not None and t.get_device() != index:
-            raise TypeError(f"need tensors on the current device, cuda:{index}, got {t.device}")
+def _bad(t, dtype, index, name):
+    """Why a tensor was refused: the calls below look at dtype, device and layout in one expression and come here only then."""
+    _dev(t, dtype, name)
+    raise TypeError(f"{name}: need a tensor on the current device, cuda:{index}, where the call enqueues its work, got {t.device}")
 
 
 def w4a8_add_rmsnorm_quantize(x, weight, eps, residual=None, group=GROUP, sum_out=None, h_out=None, out=None, stream=None):
     """x, residual bf16 [M,K], weight bf16 [K] -> (s, qa int8 [M,K], sa fp16 [M], asum int32 [M,K/group]): s = x + residual in
     bf16 (x itself without a residual), the rest w4a8_quantize_act of its root-mean-square norm times weight.
     sum_out may be x or residual; h_out receives the normed row in bf16; out = (qa, sa, asum)."""
-    _dev(x, torch.bfloat16, "x"), _dev(weight, torch.bfloat16, "weight")
-    M, K = x.shape
-    if weight.shape != (K,) or (residual is not None and residual.shape != x.shape):
+    index, bf16 = torch._C._cuda_getDevice(), torch.bfloat16
+    if not (x.dtype is bf16 and x.get_device() == index and x.is_contiguous()):
+        _bad(x, bf16, index, "x")
+    if not (weight.dtype is bf16 and weight.get_device() == index and weight.is_contiguous()):
+        _bad(weight, bf16, index, "weight")
+    shape = x.shape
+    M, K = shape
+    if weight.shape != (K,):
         raise W4A8Error(ERR_SHAPE, "w4a8_add_rmsnorm_quantize")
-    total = x
+    total, r_ptr, s_ptr, h_ptr = x, None, None, None
     if residual is not None:
-        _dev(residual, torch.bfloat16, "residual")
-        total = torch.empty_like(x) if sum_out is None else _dev(sum_out, torch.bfloat16, "sum_out")
-    if out is None:
-        out = (torch.empty((M, K), dtype=torch.int8, device=x.device), torch.empty((M,), dtype=torch.float16, device=x.device),
-               torch.empty((M, max(K // group, 0)), dtype=torch.int32, device=x.device))
-    qa, sa, asum = out
-    _dev(qa, torch.int8, "qa"), _dev(sa, torch.float16, "sa"), _dev(asum, torch.int32, "asum")
+        total = torch.empty_like(x) if sum_out is None else sum_out
+        for t, name in ((residual, "residual"), (total, "sum_out")):
+            if not (t.dtype is bf16 and t.get_device() == index and t.is_contiguous()):
+                _bad(t, bf16, index, name)
+            if t.shape != shape:
+                raise W4A8Error(ERR_SHAPE, "w4a8_add_rmsnorm_quantize")
+        r_ptr, s_ptr = residual.data_ptr(), total.data_ptr()
     if h_out is not None:
-        _dev(h_out, torch.bfloat16, "h_out")
-    if (total.shape != x.shape or qa.shape != x.shape or sa.shape != (M,) or asum.numel() != M * (K // group) or
-            (h_out is not None and h_out.shape != x.shape)):
-        raise W4A8Error(ERR_SHAPE, "w4a8_add_rmsnorm_quantize")
-    _here(x, weight, residual, total, h_out, qa, sa, asum)
-    _check(lib().w4a8_add_rmsnorm_quantize(x.data_ptr(), _ptr(residual), weight.data_ptr(), eps, M, K, group,
-                                           total.data_ptr() if residual is not None else None, _ptr(h_out), qa.data_ptr(),
-                                           sa.data_ptr(), asum.data_ptr(), _stream(stream)), "w4a8_add_rmsnorm_quantize")
+        if not (h_out.dtype is bf16 and h_out.get_device() == index and h_out.is_contiguous()):
+            _bad(h_out, bf16, index, "h_out")
+        if h_out.shape != shape:
+            raise W4A8Error(ERR_SHAPE, "w4a8_add_rmsnorm_quantize")
+        h_ptr = h_out.data_ptr()
+    if out is None:
+        qa = torch.empty((M, K), dtype=torch.int8, device=x.device)
+        sa = torch.empty((M,), dtype=torch.float16, device=x.device)
+        asum = torch.empty((M, max(K // group, 0)), dtype=torch.int32, device=x.device)
+    else:
+        qa, sa, asum = out
+        for t, dtype, n, name in ((qa, torch.int8, M * K, "qa"), (sa, torch.float16, M, "sa"), (asum, torch.int32, M * (K // group), "asum")):
+            if not (t.dtype is dtype and t.get_device() == index and t.is_contiguous()):
+                _bad(t, dtype, index, name)
+            if t.numel() != n:
+                raise W4A8Error(ERR_SHAPE, "w4a8_add_rmsnorm_quantize")
+    code = (_lib or lib()).w4a8_add_rmsnorm_quantize(x.data_ptr(), r_ptr, weight.data_ptr(), eps, M, K, group, s_ptr, h_ptr, qa.data_ptr(),
+                                                     sa.data_ptr(), asum.data_ptr(), _stream(stream))
+    if code:
+        raise W4A8Error(code, "w4a8_add_rmsnorm_quantize")
     return total, qa, sa, asum
 
 
@@ -378,6 +393,7 @@ class KV8Cache:
         self._struct = _KV8Struct(k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
                                   self.num_blocks, self.heads, self.dim, self.block)
         self._address = ctypes.addressof(self._struct)
+        self.device_index = k_codes.get_device()
 
     @classmethod
     def empty(cls, num_blocks, heads, dim, block=64, device="cuda"):
@@ -395,16 +411,18 @@ def new_kv8_workspace(cache, stream=None):
     nbytes = w4a8_kv8_workspace_bytes(cache.dim)
     if nbytes == 0:
         raise W4A8Error(ERR_SHAPE, "w4a8_kv8_workspace_bytes")
-    _here(cache.k_codes)
+    if cache.device_index != torch._C._cuda_getDevice():
+        _bad(cache.k_codes, torch.int8, torch._C._cuda_getDevice(), "k_codes")
     ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.k_codes.device)
     _check(lib().w4a8_workspace_init(_ptr(ws), nbytes, _stream(stream)), "w4a8_workspace_init")
     return ws
 
 
-def _heads_view(t, heads, dim, name):
+def _heads_view(t, heads, dim, index, name):
     """The row stride of a bf16 CUDA tensor [tokens, heads, dim] whose rows are contiguous (a column range of a wider matrix, say)."""
-    if not (t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 3):
-        raise TypeError(f"{name}: need a CUDA tensor [tokens, heads, dim] of bf16, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.dtype is not torch.bfloat16 or t.dim() != 3 or t.get_device() != index:
+        raise TypeError(f"{name}: need a tensor [tokens, heads, dim] of bf16 on the current device, cuda:{index}, got {t.dtype} "
+                        f"{tuple(t.shape)} on {t.device}")
     tokens, h, d = t.shape
     if d != dim or (heads is not None and h != heads):
         raise W4A8Error(ERR_SHAPE, name)
@@ -417,42 +435,55 @@ def _heads_view(t, heads, dim, name):
 def w4a8_kv8_append(cache, k, v, table, start, workspace, count=None, stream=None):
     """Appends k, v bf16 [B*T, heads, dim] (rows may be columns of a wider matrix) to the sequences whose blocks are table int32
     [B, width]: token i of sequence b to position start[b] + i, for i < count[b] (all T without count)."""
-    k_stride, v_stride = _heads_view(k, cache.heads, cache.dim, "k"), _heads_view(v, cache.heads, cache.dim, "v")
-    _dev(start, torch.int32, "start"), _dev(workspace, torch.uint8, "workspace")
-    _dev(table, torch.int32, "table")
+    index, i32 = torch._C._cuda_getDevice(), torch.int32
+    k_stride, v_stride = _heads_view(k, cache.heads, cache.dim, index, "k"), _heads_view(v, cache.heads, cache.dim, index, "v")
+    for t, dtype, name in ((table, i32, "table"), (start, i32, "start"), (workspace, torch.uint8, "workspace")):
+        if not (t.dtype is dtype and t.get_device() == index and t.is_contiguous()):
+            _bad(t, dtype, index, name)
+    if cache.device_index != index:
+        _bad(cache.k_codes, torch.int8, index, "k_codes")
     tokens = k.shape[0]
-    if table.dim() != 2 or (tokens % table.shape[0] if table.shape[0] else tokens):
+    if table.dim() != 2 or v.shape[0] != tokens:
         raise W4A8Error(ERR_SHAPE, "w4a8_kv8_append")
-    B = table.shape[0]
-    T = tokens // B if B else 0
-    if v.shape != k.shape or start.shape != (B,) or (count is not None and _dev(count, torch.int32, "count").shape != (B,)):
+    B, width = table.shape
+    if (tokens % B if B else tokens) or start.shape != (B,):
         raise W4A8Error(ERR_SHAPE, "w4a8_kv8_append")
-    _here(k, v, table, start, count, workspace, cache.k_codes)
-    _check(lib().w4a8_kv8_append(cache._address, k.data_ptr(), v.data_ptr(), k_stride, v_stride, B, T, table.data_ptr(), table.shape[1],
-                                 start.data_ptr(), _ptr(count), workspace.data_ptr(), workspace.numel(), _stream(stream)),
-           "w4a8_kv8_append")
+    c_ptr = None
+    if count is not None:
+        if not (count.dtype is i32 and count.get_device() == index and count.is_contiguous()):
+            _bad(count, i32, index, "count")
+        if count.shape != (B,):
+            raise W4A8Error(ERR_SHAPE, "w4a8_kv8_append")
+        c_ptr = count.data_ptr()
+    code = (_lib or lib()).w4a8_kv8_append(cache._address, k.data_ptr(), v.data_ptr(), k_stride, v_stride, B, tokens // B if B else 0, table.data_ptr(),
+                                           width, start.data_ptr(), c_ptr, workspace.data_ptr(), workspace.numel(), _stream(stream))
+    if code:
+        raise W4A8Error(code, "w4a8_kv8_append")
 
 
 def w4a8_kv8_attention(q, cache, table, limits, scale, workspace, out=None, stream=None):
     """out bf16 [B*T, q_heads*dim]: q bf16 [B*T, q_heads, dim] (rows may be columns of a wider matrix) over the cache; token t of
     sequence b sees positions 0 .. limits[b, t] - 1 of the blocks in table int32 [B, width]."""
-    q_stride = _heads_view(q, None, cache.dim, "q")
-    _dev(limits, torch.int32, "limits"), _dev(workspace, torch.uint8, "workspace")
-    _dev(table, torch.int32, "table")
+    index, i32 = torch._C._cuda_getDevice(), torch.int32
+    q_stride = _heads_view(q, None, cache.dim, index, "q")
     tokens, q_heads, dim = q.shape
-    if limits.dim() != 2 or table.dim() != 2 or table.shape[0] != limits.shape[0] or limits.numel() != tokens:
-        raise W4A8Error(ERR_SHAPE, "w4a8_kv8_attention")
-    B, T = limits.shape
     if out is None:
         out = torch.empty((tokens, q_heads * dim), dtype=torch.bfloat16, device=q.device)
-    else:
-        _dev(out, torch.bfloat16, "out")
-    if out.numel() != tokens * q_heads * dim:
+    for t, dtype, name in ((table, i32, "table"), (limits, i32, "limits"), (workspace, torch.uint8, "workspace"), (out, torch.bfloat16, "out")):
+        if not (t.dtype is dtype and t.get_device() == index and t.is_contiguous()):
+            _bad(t, dtype, index, name)
+    if cache.device_index != index:
+        _bad(cache.k_codes, torch.int8, index, "k_codes")
+    if limits.dim() != 2 or table.dim() != 2:
         raise W4A8Error(ERR_SHAPE, "w4a8_kv8_attention")
-    _here(q, table, limits, workspace, out, cache.k_codes)
-    _check(lib().w4a8_kv8_attention(cache._address, q.data_ptr(), q_stride, B, T, q_heads, table.data_ptr(), table.shape[1],
-                                    limits.data_ptr(), scale, out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream(stream)),
-           "w4a8_kv8_attention")
+    B, T = limits.shape
+    rows, width = table.shape
+    if rows != B or B * T != tokens or out.numel() != tokens * q_heads * dim:
+        raise W4A8Error(ERR_SHAPE, "w4a8_kv8_attention")
+    code = (_lib or lib()).w4a8_kv8_attention(cache._address, q.data_ptr(), q_stride, B, T, q_heads, table.data_ptr(), width, limits.data_ptr(), scale,
+                                              out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream(stream))
+    if code:
+        raise W4A8Error(code, "w4a8_kv8_attention")
     return out
 
 

@@ -42,7 +42,7 @@ __device__ __forceinline__ uint32_t norm2(uint32_t s, uint32_t w, float rstd) {
 // T threads per row, CACHE chunks of 8 elements per thread in registers (a longer row's rest is read again: from sum_out, which
 // may have overwritten x or r).  FAST: the quantiser's reciprocal form (see quantize_act.cu), for many rows.
 template <int T, int CACHE, bool FAST, bool ADD>
-__global__ void __launch_bounds__(T)
+__global__ void __launch_bounds__(T, FAST && T == 256 ? (CACHE <= 3 ? 5 : 3) : 1)
 add_rmsnorm_quantize_kernel(const uint4* x, const uint4* r, const uint4* __restrict__ w, float eps, int K, uint4* sum_out, uint4* h_out,
                             uint2* __restrict__ qa, uint16_t* __restrict__ sa, int32_t* __restrict__ asum) {
     ptx::pdl_launch_dependents();
@@ -163,7 +163,14 @@ cudaError_t launch_add_rmsnorm_quantize(const void* x, const void* residual, con
     const uint4 *xp = static_cast<const uint4*>(x), *rp = static_cast<const uint4*>(residual), *wp = static_cast<const uint4*>(weight);
     uint4 *sp = static_cast<uint4*>(sum_out), *hp = static_cast<uint4*>(h_out);
     uint2* qp = reinterpret_cast<uint2*>(qa);
-    if (M <= 512) return launch_norm<512, 3, false>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
+    if (K <= 1024) return launch_norm<128, 1, false>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
+    if (M <= 512) {
+        if (K <= 2048) return launch_norm<256, 1, false>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
+        if (K <= 4096) return launch_norm<512, 1, false>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
+        return launch_norm<512, 3, false>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
+    }
+    if (K <= 4096) return launch_norm<256, 2, true>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
+    if (K <= 6144) return launch_norm<256, 3, true>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
     return launch_norm<256, 6, true>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
 }
 
