@@ -32,8 +32,10 @@ struct ArCfg {
     static constexpr int JOIN = 2 * ROWS * O_PITCH * 4;
     static constexpr int W_OFF = RING > JOIN ? RING : JOIN;               // weights on their way: [warp][turn & 1][RB][lane] 16 bytes
     static constexpr int W_BYTES = RB * 512;
-    static constexpr int Q_OFF = W_OFF + AR_WARPS * 2 * W_BYTES;          // q as operand: [D / 16][RB][lane] 16 bytes (16 rows: in registers)
-    static constexpr int TOP_OFF = Q_OFF + (RB == 1 ? 0 : (D / 16) * RB * 512);           // rows' maxima where a reference moves: [warp][ROWS] float
+    static constexpr int W_END = W_OFF + AR_WARPS * 2 * W_BYTES;
+    static constexpr int Q_OFF = RB == 1 ? W_OFF : W_END;                 // q as operand: [D / 16][RB][lane] 16 bytes (16 rows: only passing through)
+    static constexpr int FACTOR_OFF = RB == 1 ? W_END : Q_OFF + (D / 16) * RB * 512;        // rows' factors: [ROWS] float
+    static constexpr int TOP_OFF = FACTOR_OFF + ROWS * 4;                 // rows' maxima where a reference moves: [warp][ROWS] float
     static constexpr int FLAG_OFF = TOP_OFF + AR_WARPS * ROWS * 4;        // whether one does: [warp][turn & 1]
     static constexpr int ML_OFF = FLAG_OFF + AR_WARPS * 8;                // at the end: references and sums of each warp's positions
     static constexpr int SMEM = ML_OFF + AR_WARPS * ROWS * 8;
@@ -76,60 +78,54 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     const int rows = a.T * a.rep, row0 = tile * C::ROWS;
     ptx::pdl_wait();
 
-    // ---- this lane's rows: limits, q as fp16, and the factor that undoes its power of two.  With 32 rows q goes to shared memory, each warp
-    // a part.
+    // ---- this lane's rows' limits; and q as fp16 operand, with the factors that undo its powers of two, through shared memory: eight rows (half a
+    // block of 16) from each of the first 2 RB warps
     int limit[RB][2];
-    float factor[RB][2];
-    uint32_t qf[RB == 1 ? KS : 1][4];
     int longest = 0, shortest = 0x7FFFFFFF;
     const int capacity = (int)min((long long)a.table_width << a.log2_block, 0x7FFFFFF0ll);
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        uint32_t q2[KS][4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int r = row0 + rb * 16 + h * 8 + g;
             limit[rb][h] = 0;
-            uint32_t w[KS * 2];
-#pragma unroll
-            for (int i = 0; i < KS * 2; ++i) w[i] = 0;
             if (r < rows) {
-                const int token = r / a.rep, head = kv_head * a.rep + r - token * a.rep;
-                const long long at = (long long)seq * a.T + token;
-                limit[rb][h] = min(max(__ldcg(a.limits + at), 0), capacity);
-                const uint16_t* src = a.q + at * a.q_stride + (long long)head * D + 16 * t;
-#pragma unroll
-                for (int i = 0; i < D / 64; ++i) {
-                    const uint4 x = __ldcg(reinterpret_cast<const uint4*>(src + 64 * i)), y = __ldcg(reinterpret_cast<const uint4*>(src + 64 * i + 8));
-                    w[8 * i] = x.x, w[8 * i + 1] = x.y, w[8 * i + 2] = x.z, w[8 * i + 3] = x.w;
-                    w[8 * i + 4] = y.x, w[8 * i + 5] = y.y, w[8 * i + 6] = y.z, w[8 * i + 7] = y.w;
-                }
+                limit[rb][h] = min(max(__ldcg(a.limits + (long long)seq * a.T + r / a.rep), 0), capacity);
                 shortest = min(shortest, limit[rb][h]);
             }
             longest = max(longest, limit[rb][h]);
-            uint32_t run = 0;
+        }
+    }
+    if (warp < 2 * RB) {
+        const int rb = warp >> 1, h = warp & 1, r = row0 + rb * 16 + h * 8 + g;
+        uint32_t w[KS * 2];
 #pragma unroll
-            for (int i = 0; i < KS * 2; ++i) run = __vmaxu2(run, w[i] & 0x7FFF7FFFu);
-            run = max(run & 0xFFFFu, run >> 16);
-            run = max(run, __shfl_xor_sync(0xFFFFFFFFu, run, 1));
-            run = max(run, __shfl_xor_sync(0xFFFFFFFFu, run, 2));
-            const int e = kv8_row_exp(run);
-            const float up = kv8_pow2(e);
-            factor[rb][h] = a.scale_log2 * kv8_pow2(-e);
+        for (int i = 0; i < KS * 2; ++i) w[i] = 0;
+        if (r < rows) {
+            const int token = r / a.rep, head = kv_head * a.rep + r - token * a.rep;
+            const uint16_t* src = a.q + ((long long)seq * a.T + token) * a.q_stride + (long long)head * D + 16 * t;
 #pragma unroll
-            for (int i = 0; i < KS; ++i) {
-                q2[i][h] = kv8_pack_half2(__uint_as_float(w[2 * i] << 16) * up, __uint_as_float(w[2 * i] & 0xFFFF0000u) * up);
-                q2[i][2 + h] = kv8_pack_half2(__uint_as_float(w[2 * i + 1] << 16) * up, __uint_as_float(w[2 * i + 1] & 0xFFFF0000u) * up);
+            for (int i = 0; i < D / 64; ++i) {
+                const uint4 x = __ldcg(reinterpret_cast<const uint4*>(src + 64 * i)), y = __ldcg(reinterpret_cast<const uint4*>(src + 64 * i + 8));
+                w[8 * i] = x.x, w[8 * i + 1] = x.y, w[8 * i + 2] = x.z, w[8 * i + 3] = x.w;
+                w[8 * i + 4] = y.x, w[8 * i + 5] = y.y, w[8 * i + 6] = y.z, w[8 * i + 7] = y.w;
             }
         }
+        uint32_t run = 0;
+#pragma unroll
+        for (int i = 0; i < KS * 2; ++i) run = __vmaxu2(run, w[i] & 0x7FFF7FFFu);
+        run = max(run & 0xFFFFu, run >> 16);
+        run = max(run, __shfl_xor_sync(0xFFFFFFFFu, run, 1));
+        run = max(run, __shfl_xor_sync(0xFFFFFFFFu, run, 2));
+        const int e = kv8_row_exp(run);
+        const float up = kv8_pow2(e);
+        if (t == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(smem + C::FACTOR_OFF + (rb * 16 + h * 8 + g) * 4), "f"(a.scale_log2 * kv8_pow2(-e)) : "memory");
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
-            if (RB == 1) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) qf[i % (RB == 1 ? KS : 1)][k] = q2[i][k];
-            } else if (i % AR_WARPS == warp) {
-                ptx::sts128u(smem + C::Q_OFF + ((i * RB + rb) * 32 + lane) * 16, q2[i][0], q2[i][1], q2[i][2], q2[i][3]);
-            }
+            // words h and 2 + h of the lane's four
+            const uint32_t at = smem + C::Q_OFF + ((i * RB + rb) * 32 + lane) * 16 + 4 * h;
+            asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(kv8_pack_half2(__uint_as_float(w[2 * i] << 16) * up, __uint_as_float(w[2 * i] & 0xFFFF0000u) * up)) : "memory");
+            asm volatile("st.shared.u32 [%0], %1;" ::"r"(at + 8), "r"(kv8_pack_half2(__uint_as_float(w[2 * i + 1] << 16) * up, __uint_as_float(w[2 * i + 1] & 0xFFFF0000u) * up)) : "memory");
         }
     }
     longest = __reduce_max_sync(0xFFFFFFFFu, longest);
@@ -187,6 +183,20 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
 #pragma unroll
     for (int i = 0; i < C::STAGES - 1; ++i) issue(i);
     __syncthreads();                                         // q and flags are there
+    float factor[RB][2];
+    uint32_t qf[RB == 1 ? KS : 1][4];                        // 16 rows: q stays in registers
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) factor[rb][h] = __uint_as_float(ptx::lds32(smem + C::FACTOR_OFF + (rb * 16 + h * 8 + g) * 4));
+    if (RB == 1) {
+#pragma unroll
+        for (int i = 0; i < (RB == 1 ? KS : 1); ++i) {
+            const uint4 y = ptx::lds128(smem + C::Q_OFF + (i * 32 + lane) * 16);
+            qf[i][0] = y.x, qf[i][1] = y.y, qf[i][2] = y.z, qf[i][3] = y.w;
+        }
+        __syncthreads();                                     // weights follow in its place
+    }
 
     float o[RB][NB][4];
     float ref[RB][2], sum[RB][2];
