@@ -63,6 +63,16 @@ __device__ __forceinline__ uint32_t chunk_at(int r, int p) {
     return (uint32_t)(line * 128 + ((piece ^ turn) << 4));
 }
 
+// From a place to others, a chunk's first byte being a multiple of 128 (spelled out: eight rows on keep the turn, and so on, which the compiler does
+// not see; with an evaluation of chunk_at for each access the loop had a fifth more instructions)
+template <int D>
+__device__ __forceinline__ constexpr uint32_t rows_on8() { return D == 128 ? 1024u : 512u; }
+template <int D>
+__device__ __forceinline__ uint32_t row_on1_from_even(uint32_t at) { return D == 128 ? (at + 128u) ^ 64u : at ^ 64u; }
+__device__ __forceinline__ uint32_t pieces_on4(uint32_t at) { return at ^ 64u; }                   // D = 128
+template <int D>
+__device__ __forceinline__ uint32_t bytes_on512(uint32_t at, int j) { return D == 128 && (j & 1) ? (at ^ 64u) + 512u * j : at + 512u * j; }
+
 template <int D, int RB>
 __global__ void __launch_bounds__(AR_WARPS * 32, (ArCfg<D, RB>::CTAS))
 kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
@@ -161,6 +171,8 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     int base = 0;
     const uint32_t ring = smem + warp * (C::STAGES * C::STAGE), other_ring = smem + (warp ^ 1) * (C::STAGES * C::STAGE);
     int slot_in = 0;
+    const uint32_t in_at = chunk_at<D>(lane / (D / 16), lane % (D / 16)), k_at = chunk_at<D>(g, t);
+    const uint32_t v_at = C::K_BYTES + (D == 128 ? chunk_at<D>(2 * t, 4 * side + (g >> 1)) + 8 * (g & 1) : chunk_at<D>(2 * t, 2 * side + (g >> 2)) + 4 * (g & 3));
     auto issue = [&](int i) {
         if (i < turns) {
             const int number = __shfl_sync(0xFFFFFFFFu, i - base < 32 ? cur.number : nxt.number, i & 31);
@@ -168,12 +180,11 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
                 const int inside = ((first + 4 * i) & ((1 << chunk_shift) - 1)) * AR_CHUNK;
                 const size_t at = ((((size_t)number * a.kv_heads + kv_head) << a.log2_block) + inside) * D + lane * 16;
                 const int8_t *k = a.k_codes + at, *v = a.v_codes + at;
-                const uint32_t dst = ring + slot_in * C::STAGE;
+                const uint32_t dst = ring + slot_in * C::STAGE + in_at;
 #pragma unroll
                 for (int j = 0; j < C::K_BYTES / 512; ++j) {
-                    const int idx = j * 32 + lane, r = idx / (D / 16), p = idx % (D / 16);
-                    cp_async16(dst + chunk_at<D>(r, p), k + j * 512);
-                    cp_async16(dst + C::K_BYTES + chunk_at<D>(r, p), v + j * 512);
+                    cp_async16(bytes_on512<D>(dst, j), k + j * 512);
+                    cp_async16(bytes_on512<D>(dst, j) + C::K_BYTES, v + j * 512);
                 }
             }
         }
@@ -221,7 +232,7 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
         const int number = __shfl_sync(0xFFFFFFFFu, cur.number, i & 31);
         const uint32_t scales = __shfl_sync(0xFFFFFFFFu, cur.scales, i & 31);
         const int key0 = (first + 4 * i) * AR_CHUNK;
-        const uint32_t kst = ring + slot * C::STAGE;
+        const uint32_t kst = ring + slot * C::STAGE + k_at;
         // ---- scores of this warp's 16 positions: columns 8 n + 2 t, + 1
         float s[RB][2][4];
 #pragma unroll
@@ -230,7 +241,8 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
             for (int n = 0; n < 2; ++n) s[rb][n][0] = s[rb][n][1] = s[rb][n][2] = s[rb][n][3] = 0.0f;
 #pragma unroll
         for (int i4 = 0; i4 < D / 64; ++i4) {
-            const uint4 x0 = ptx::lds128(kst + chunk_at<D>(g, t + 4 * i4)), x1 = ptx::lds128(kst + chunk_at<D>(8 + g, t + 4 * i4));
+            const uint32_t at = i4 ? pieces_on4(kst) : kst;
+            const uint4 x0 = ptx::lds128(at), x1 = ptx::lds128(at + rows_on8<D>());
             const uint32_t w[2][4] = {{x0.x, x0.y, x0.z, x0.w}, {x1.x, x1.y, x1.z, x1.w}};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -360,7 +372,7 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
         // NB g + j of the half
 #pragma unroll
         for (int turn = 0; turn < 2; ++turn) {
-            const uint32_t vst = (turn ? other_ring : ring) + slot * C::STAGE + C::K_BYTES;
+            const uint32_t vst = (turn ? other_ring : ring) + slot * C::STAGE + v_at, vst1 = row_on1_from_even<D>(vst);
             if (turn) {
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb) {
@@ -371,12 +383,12 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
             uint32_t v[4][NB / 4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int r = 2 * t + (k & 1) + 8 * (k >> 1);
+                const uint32_t at = (k & 1 ? vst1 : vst) + (k >> 1) * rows_on8<D>();
                 if (D == 128) {
-                    const uint2 x = ptx::lds64(vst + chunk_at<D>(r, 4 * side + (g >> 1)) + 8 * (g & 1));
+                    const uint2 x = ptx::lds64(at);
                     v[k][0] = x.x, v[k][NB / 4 - 1] = x.y;
                 } else {
-                    v[k][0] = ptx::lds32(vst + chunk_at<D>(r, 2 * side + (g >> 2)) + 4 * (g & 3));
+                    v[k][0] = ptx::lds32(at);
                 }
             }
 #pragma unroll
