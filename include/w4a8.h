@@ -263,12 +263,13 @@ w4a8_status w4a8_streaming_mask(int views, int frames, int tokens_per_frame, uin
  *   (qa, sa, asum) = w4a8_quantize_act of h, bit-exact given h: the operands of w4a8_gemm
  *   x         device, bf16 [M,K] row-major, 16-byte aligned, like residual, sum and h
  *   residual  the same shape, or NULL
- *   weight    device, bf16 [K], 16-byte aligned;  eps >= 0
+ *   weight    device, bf16 [K], 16-byte aligned;  eps >= 0 (with 0, a row of zeros has no norm: its results are undefined)
  *   sum       receives s; required with a residual and may be the same buffer as x or as the residual (a thread reads what
  *             it then overwrites); NULL without a residual
  *   h         receives h; may be NULL; not one of the other buffers
  *   qa, sa, asum   as for w4a8_quantize_act
- * Not-a-number and infinity in a row: that row's results are undefined, as for w4a8_quantize_act.
+ * Not-a-number and infinity in a row, and a sum of squares past the fp32 range: that row's results are undefined, as for
+ * w4a8_quantize_act.
  */
 w4a8_status w4a8_add_rmsnorm_quantize(const void* x_bf16, const void* residual_bf16, const void* weight_bf16, float eps,
                                       int M, int K, int group, void* sum_bf16, void* h_bf16,
@@ -331,8 +332,10 @@ w4a8_status w4a8_kv8_append(const w4a8_kv8_cache* cache, const void* k_bf16, con
  *   limits    device, int32 [B][T];  out  device, bf16 [B T][q_heads dim], 16-byte aligned
  *   workspace at least w4a8_kv8_workspace_bytes(dim) bytes, 256-byte aligned, initialised once; the same rules as for
  *             w4a8_gemm, with whose calls it may be shared on one stream.  Enough for any call of this dim; 0: unsupported dim
+ * Up to 32 rows (tokens x query heads of a group) the cache streams through the kernel for few rows, above through the tcgen05
+ * kernel; where row tiles are fewer than the SMs hold, the keys are split as well and a second kernel joins the sums.
  * Results are run-to-run deterministic.  W4A8_ERR_SHAPE also for q_heads not a multiple of heads, more than 65535 / heads
- * sequences, 2^31 or more rows T q_heads / heads, or B x T >= 2^31.
+ * sequences, B x T >= 2^31, T q_heads / heads > 2^31 - 512, or 2^30 tiles of 256 rows and more.
  */
 size_t w4a8_kv8_workspace_bytes(int dim);
 w4a8_status w4a8_kv8_attention(const w4a8_kv8_cache* cache, const void* q_bf16, long long q_stride, int B, int T, int q_heads,

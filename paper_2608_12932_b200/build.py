@@ -46,8 +46,10 @@ def check_ptxas(report):
             limit = 0                             # whose roles have few registers each: a spill sits in a loop
         if spill > limit and "gemm_" in name:
             problems.append(f"{name}: {spill} bytes of spill stores")
-        if "gemm_tcgen05" in name or "gemm_tcshort" in name:      # 512 and 640 threads share the 64 K registers
-            want = 128 if "gemm_tcgen05" in name else 96
+        if spill > 64 and ("kv8_attend" in name or "rmsnorm" in name or "kv8_append" in name or "kv8_combine" in name):
+            problems.append(f"{name}: {spill} bytes of spill stores")
+        if "gemm_tcgen05" in name or "gemm_tcshort" in name or "kv8_attend_tiles" in name:      # 512 and 640 threads share the 64 K registers
+            want = 96 if "gemm_tcshort" in name else 128
             if regs != want:
                 problems.append(f"{name}: {regs} registers at launch, setmaxnreg budget assumes {want}")
     if problems:

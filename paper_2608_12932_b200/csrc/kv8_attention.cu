@@ -92,7 +92,7 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     // block of 16) from each of the first 2 RB warps
     int limit[RB][2];
     int longest = 0, shortest = 0x7FFFFFFF;
-    const int capacity = (int)min((long long)a.table_width << a.log2_block, 0x7FFFFFF0ll);
+    const int capacity = (int)min((long long)a.table_width << a.log2_block, 0x7FFFFF00ll);
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
