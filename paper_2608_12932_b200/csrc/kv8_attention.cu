@@ -1,8 +1,8 @@
 // Attention over the 8-bit key/value cache for few rows: single tokens and draft blocks (definition and number formats in
 // kv8_attention.cuh).
 //
-// kv8_attend_rows_kernel: one CTA per (sequence, key head, row tile, slice of the keys).  A row tile is 16 or 32 (token, head)
-// rows of one key head's group, so a group's heads share what is read of the cache.  Two pairs of warps walk chunks of 2 x 16 positions,
+// kv8_attend_rows_kernel: one CTA per (sequence, key head, slice of the keys) for the 16 or 32 (token, head) rows of the key
+// head's group, so a group's heads share what is read of the cache.  Two pairs of warps walk chunks of 2 x 16 positions,
 // each pair with its own running sums: a warp fetches 16 positions' codes (16-byte asynchronous copies into a ring of its own), forms their
 // scores and weights, hands the weights to its partner through shared memory, and multiplies the values of all 32 positions for its half of the
 // channels.  So a warp keeps half a tile's sums: a warp that keeps all of them needs 255 registers at 32 rows, and two warps
@@ -84,8 +84,8 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     ptx::pdl_launch_dependents();
     const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int pair = warp >> 1, side = warp & 1;
-    const int tile = blockIdx.x / a.slices, slice = blockIdx.x - tile * a.slices, kv_head = blockIdx.z % a.kv_heads, seq = blockIdx.z / a.kv_heads;
-    const int rows = a.T * a.rep, row0 = tile * C::ROWS;
+    const int slice = blockIdx.x, kv_head = blockIdx.z % a.kv_heads, seq = blockIdx.z / a.kv_heads;
+    const int rows = a.T * a.rep;
     ptx::pdl_wait();
 
     // ---- this lane's rows' limits; and q as fp16 operand, with the factors that undo its powers of two, through shared memory: eight rows (half a
@@ -97,7 +97,7 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int r = row0 + rb * 16 + h * 8 + g;
+            const int r = rb * 16 + h * 8 + g;
             limit[rb][h] = 0;
             if (r < rows) {
                 limit[rb][h] = min(max(__ldcg(a.limits + (long long)seq * a.T + r / a.rep), 0), capacity);
@@ -107,7 +107,7 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
         }
     }
     if (warp < 2 * RB) {
-        const int rb = warp >> 1, h = warp & 1, r = row0 + rb * 16 + h * 8 + g;
+        const int rb = warp >> 1, h = warp & 1, r = rb * 16 + h * 8 + g;
         uint32_t w[KS * 2];
 #pragma unroll
         for (int i = 0; i < KS * 2; ++i) w[i] = 0;
@@ -437,10 +437,10 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
         }
     }
     __syncthreads();
-    const size_t unit = ((size_t)blockIdx.z * a.tiles + tile) * a.slices + slice;
+    const size_t unit = (size_t)blockIdx.z * a.slices + slice;
     for (int idx = tid; idx < C::ROWS * (D / 4); idx += AR_WARPS * 32) {
-        const int r = idx / (D / 4), d = (idx % (D / 4)) * 4, row = row0 + r;
-        if (row >= rows) break;
+        const int r = idx / (D / 4), d = (idx % (D / 4)) * 4;
+        if (r >= rows) break;
         float m = -INFINITY;
 #pragma unroll
         for (int w = 0; w < 2; ++w) m = fmaxf(m, ml[2 * w * C::ROWS + r].x);
@@ -463,7 +463,7 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
             if (d == 0) a.part_ml[unit * C::ROWS + r] = make_float2(m, l);
         } else {
             const float inv = l == 0.0f ? 0.0f : __fdividef(1.0f, l);
-            const int token = row / a.rep, head = kv_head * a.rep + row - token * a.rep;
+            const int token = r / a.rep, head = kv_head * a.rep + r - token * a.rep;
             uint2* dst = reinterpret_cast<uint2*>(a.out + (((long long)seq * a.T + token) * a.q_heads + head) * D + d);
             *dst = make_uint2(ptx::pack_bf16x2(x.x * inv, x.y * inv), ptx::pack_bf16x2(x.z * inv, x.w * inv));
         }
@@ -576,7 +576,7 @@ cudaError_t launch_rows(const AttendArgs& a, int B, cudaStream_t stream) {
         ready[dev] = true;
     }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)a.slices * (unsigned)a.tiles, 1, (unsigned)(B * a.kv_heads));
+    cfg.gridDim = dim3((unsigned)a.slices, 1, (unsigned)(B * a.kv_heads));
     cfg.blockDim = dim3(AR_WARPS * 32, 1, 1);
     cfg.dynamicSmemBytes = C::SMEM;
     cfg.stream = stream;

@@ -41,12 +41,11 @@ struct TcCfg {
     static constexpr uint32_t S_COL = 0, O_COL = 256;                            // tensor memory: scores 2 x 128 columns, sums 2 x 128
 };
 
-#ifndef TC_POLY
-#define TC_POLY 2
-#endif
+constexpr int TC_POLY = 2;                                    // of eight pairs of exponentials, those taken by the polynomial
 // 2^x and 2^y without the special-function unit: x = n + f with n the nearest integer (which lands in the low mantissa bits of x + 1.5 2^23), 2^f
 // on [-1/2, 1/2] by the polynomial of degree 4 with the smallest largest relative error, 2.6e-6 (Remez), n added to the exponent.
-// Below -126, 2^-126 or less; not-a-number stays no number that anything finite is made of.
+// Below -126, and for not-a-number, a denormal number of nearly 2^-126: nothing as an fp16 weight, nothing in a sum that has a reference (and a row
+// that is not a number has its other weights to say so).
 __device__ __forceinline__ float2 exp2_poly2(float x, float y) {
     constexpr float C4 = 0.009570102207362652f, C3 = 0.05591785907745361f, C2 = 0.240247443318367f, C1 = 0.6931217908859253f, C0 = 0.9999992847442627f;
     constexpr float MAGIC = 12582912.0f;
@@ -257,7 +256,7 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
                             const int at = (4 * c + b) * 16 + 2 * i;
                             const float x = __uint_as_float(s[at >> 5][at & 31]), y = __uint_as_float(s[at >> 5][(at & 31) + 1]);
                             float2 w;
-                            if (i % 8 < TC_POLY)
+                            if (i < TC_POLY)
                                 w = exp2_poly2(x, y);
                             else
                                 w = make_float2(kv8_ex2(x), kv8_ex2(y));
@@ -278,6 +277,7 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
             if (ok && n > 0) ok = ptx::warp_mbar_wait_suspend(bar(C::OF + h), 0, abort_flag);
             if (ok) {
                 ptx::tc_fence_after_sync();
+                if (ref == -INFINITY && sum == sum) sum = 0.0f;               // no key at all: what the polynomial makes of -infinity is left
                 const float inv = sum == 0.0f ? 0.0f : __fdividef(1.0f, sum);
                 const size_t part = (((size_t)unit * a.tiles + tile) * a.slices + slice) * TC_ROWS + (size_t)(row - row0);
                 uint16_t* dst = a.out + (((long long)seq * a.T + token) * a.q_heads + head) * D;

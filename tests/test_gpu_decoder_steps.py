@@ -438,3 +438,29 @@ def test_cache_refusals():
     B.w4a8_kv8_append(c.dev, k[:0], k[:0], tt, start, c.ws)
     torch.cuda.synchronize()
     c.check()
+
+
+@pytest.mark.parametrize("T", [1, 8, 150])
+@pytest.mark.parametrize("dim,keys", [(64, 90), (128, 900)])
+def test_rows_without_a_key_beside_large_value_scales(T, dim, keys):
+    """Their sums hold nothing, also where the reciprocals of the scales are small; the other rows' do not gain from what is masked."""
+    _, c, table, q = attend_case(T + dim, 2, T, 1, 4, dim, 16, keys, v_scale=(20000.0, 60000.0))
+    limits = causal([keys, keys - 50], T)
+    limits[:, ::3] = 0
+    got = c.check_attend(q, table, limits)
+    assert (got[limits == 0] == 0).all()
+
+
+@pytest.mark.parametrize("T", [8, 150])
+def test_many_blocks_of_scale_zero_with_next_to_no_weight(T):
+    """Values of zero whose keys score far below the others: they change neither sum nor result, however many there are."""
+    _, c, table, q = attend_case(T, 1, T, 1, 4, 64, 16, 120000)
+    q[:] = bf16(np.ones(q.shape))
+    c.k[:] = -127                                             # scores of -50.8, the first block's 0.4
+    c.ks[:] = onp.f64_to_fp16_bits(np.float64(0.05))
+    c.vs[:], c.v[:] = 0, 0
+    first = table[0, 0]
+    c.k[first], c.v[first], c.vs[first] = 1, 100, onp.f64_to_fp16_bits(np.float64(60000.0))
+    c.upload()
+    got = c.check_attend(q, table, np.full((1, T), 120000))
+    assert np.abs(got / 6e6 - 1).max() <= 2.0 ** -7
