@@ -18,7 +18,7 @@
 namespace w4a8 {
 namespace {
 
-constexpr int APPEND_THREADS = 128;
+constexpr int APPEND_FEW = 128, APPEND_MANY = 512;           // threads per CTA
 
 struct AppendArgs {
     const uint4 *k, *v;
@@ -43,9 +43,9 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t codes, float s_old, float 
     return o;
 }
 
-// CH: 16-byte pieces of new values per thread
-template <int CH>
-__global__ void __launch_bounds__(APPEND_THREADS)
+// THREADS per CTA, CH 16-byte pieces of new values per thread
+template <int THREADS, int CH>
+__global__ void __launch_bounds__(THREADS)
 kv8_append_kernel(const AppendArgs a) {
     ptx::pdl_launch_dependents();
     const int tid = threadIdx.x, seq = blockIdx.z, head = blockIdx.y >> 1;
@@ -65,15 +65,6 @@ kv8_append_kernel(const AppendArgs a) {
     if (first >= end || count == 0) return;
     const int lo = (int)(max((long long)start, first) - first), hi = (int)(min(end, first + block) - first);     // slots of the new tokens
     const int number = index < a.table_width ? __ldcg(a.table + (size_t)seq * a.table_width + index) : -1;
-    if ((unsigned)number >= (unsigned)a.num_blocks) {
-        if (tid == 0) *a.status = W4A8_ERR_INDEX;
-        return;
-    }
-    const size_t at = (size_t)number * a.heads + head;
-    const size_t codes_at = at * (size_t)(block * a.pieces);                            // in pieces of 8 codes
-    uint2* codes = reinterpret_cast<uint2*>(is_v ? a.v_codes : a.k_codes) + codes_at;
-    uint16_t* scale = (is_v ? a.v_scales : a.k_scales) + at;
-    const uint32_t old_bits = lo > 0 ? (uint32_t)__ldcg(scale) : 0u;
     const long long stride = is_v ? a.v_stride : a.k_stride;
     // token of slot j: (seq T + first + j - start)
     const uint4* src = (is_v ? a.v : a.k) + ((long long)seq * a.T + first - start) * stride + (long long)head * a.pieces;
@@ -83,24 +74,34 @@ kv8_append_kernel(const AppendArgs a) {
     uint32_t run = 0;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int p = n_lo + tid + i * APPEND_THREADS;
+        const int p = n_lo + tid + i * THREADS;
         if (p < n_hi) x[i] = __ldcg(src + (long long)(p >> log2_pieces) * stride + (p & (a.pieces - 1)));
     }
+    // (the new values are on their way while the table is read, and the old scale)
+    if ((unsigned)number >= (unsigned)a.num_blocks) {
+        if (tid == 0) *a.status = W4A8_ERR_INDEX;
+        return;
+    }
+    const size_t at = (size_t)number * a.heads + head;
+    const size_t codes_at = at * (size_t)(block * a.pieces);                            // in pieces of 8 codes
+    uint2* codes = reinterpret_cast<uint2*>(is_v ? a.v_codes : a.k_codes) + codes_at;
+    uint16_t* scale = (is_v ? a.v_scales : a.k_scales) + at;
+    const uint32_t old_bits = lo > 0 ? (uint32_t)__ldcg(scale) : 0u;
 #pragma unroll
     for (int i = 0; i < CH; ++i)
-        if (n_lo + tid + i * APPEND_THREADS < n_hi) run = absmax_bits_bf16x8(x[i], run);
+        if (n_lo + tid + i * THREADS < n_hi) run = absmax_bits_bf16x8(x[i], run);
     uint32_t mx = __reduce_max_sync(0xFFFFFFFFu, max(run & 0xFFFFu, run >> 16));
-    __shared__ uint32_t warp_max[APPEND_THREADS / 32];
+    __shared__ uint32_t warp_max[THREADS / 32];
     if ((tid & 31) == 0) warp_max[tid >> 5] = mx;
     __syncthreads();                                         // every thread has read the old scale, too
 #pragma unroll
-    for (int i = 0; i < APPEND_THREADS / 32; ++i) mx = max(mx, warp_max[i]);
+    for (int i = 0; i < THREADS / 32; ++i) mx = max(mx, warp_max[i]);
     // scales are not negative: their bits order like their values
     const uint32_t bits = max((uint32_t)__half_as_ushort(row_scale_from_amax_bits(mx)), old_bits);
     const float s = __half2float(__ushort_as_half((uint16_t)bits));
     if (bits != old_bits) {
         const float s_old = __half2float(__ushort_as_half((uint16_t)old_bits));
-        for (int p = tid; p < n_lo; p += APPEND_THREADS) {
+        for (int p = tid; p < n_lo; p += THREADS) {
             const uint2 q = codes[p];
             codes[p] = make_uint2(rescale4(q.x, s_old, s), rescale4(q.y, s_old, s));
         }
@@ -110,7 +111,7 @@ kv8_append_kernel(const AppendArgs a) {
     const float rinv = s != 0.0f ? __frcp_rn(s) : 0.0f;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int p = n_lo + tid + i * APPEND_THREADS;
+        const int p = n_lo + tid + i * THREADS;
         if (p >= n_hi) continue;
         uint2 o = make_uint2(0u, 0u);
         if (s != 0.0f) {
@@ -154,7 +155,6 @@ cudaError_t launch_kv8_append(const w4a8_kv8_cache& c, const void* k, const void
     cudaLaunchConfig_t cfg = {};
     // a run of T tokens touches at most this many blocks, wherever it starts
     cfg.gridDim = dim3((unsigned)(((long long)T + c.block - 2) / c.block + 1), (unsigned)(2 * c.heads), (unsigned)B);
-    cfg.blockDim = dim3(APPEND_THREADS, 1, 1);
     cfg.stream = stream;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -162,12 +162,11 @@ cudaError_t launch_kv8_append(const w4a8_kv8_cache& c, const void* k, const void
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     const int most = (T < c.block ? T : c.block) * a.pieces;                     // pieces of new values in one block
-    const int per = (most + APPEND_THREADS - 1) / APPEND_THREADS;
-    if (per <= 1) return cudaLaunchKernelEx(&cfg, kv8_append_kernel<1>, a);
-    if (per <= 2) return cudaLaunchKernelEx(&cfg, kv8_append_kernel<2>, a);
-    if (per <= 4) return cudaLaunchKernelEx(&cfg, kv8_append_kernel<4>, a);
-    if (per <= 8) return cudaLaunchKernelEx(&cfg, kv8_append_kernel<8>, a);
-    return cudaLaunchKernelEx(&cfg, kv8_append_kernel<16>, a);
+    const int threads = most > 2 * APPEND_FEW ? APPEND_MANY : APPEND_FEW;
+    const int per = (most + threads - 1) / threads;
+    cfg.blockDim = dim3((unsigned)threads, 1, 1);
+    if (threads == APPEND_FEW) return cudaLaunchKernelEx(&cfg, per == 1 ? kv8_append_kernel<APPEND_FEW, 1> : kv8_append_kernel<APPEND_FEW, 2>, a);
+    return cudaLaunchKernelEx(&cfg, per == 1 ? kv8_append_kernel<APPEND_MANY, 1> : per == 2 ? kv8_append_kernel<APPEND_MANY, 2> : kv8_append_kernel<APPEND_MANY, 4>, a);
 }
 
 }  // namespace w4a8

@@ -15,6 +15,7 @@
 // A step's products cost 2 x 128 x 128 x D x 2 multiply-adds (2048 cycles of the tensor pipe at D = 128), its 32768 exponentials as much of the
 // special-function units, its operands and the conversion as much of shared memory's bandwidth: none of the three bounds it alone.
 #include "kv8_attention.cuh"
+#include "quant_common.cuh"
 
 namespace w4a8 {
 namespace {
@@ -118,11 +119,13 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
     const uint32_t tmem = *tmem_holder;
     ptx::pdl_wait();
 
-    int limit = 0, token = 0, head = 0;
+    int limit = 0;
     const int row = row0 + tid;                               // threads 0..255: this thread's row
+    long long q_at = -1, out_at = -1;                         // where it begins in q and in out
     if (tid < TC_ROWS && row < rows) {
-        token = row / a.rep;
-        head = kv_head * a.rep + row - token * a.rep;
+        const int token = row / a.rep, head = kv_head * a.rep + row - token * a.rep;
+        q_at = ((long long)seq * a.T + token) * a.q_stride + (long long)head * D;
+        out_at = (((long long)seq * a.T + token) * a.q_heads + head) * D;
         limit = min(max(__ldcg(a.limits + (long long)seq * a.T + token), 0), capacity);
     }
     if (tid < TC_ROWS) {
@@ -138,35 +141,34 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         const int h = warp >> 2;
         if (h < halves) {
-            // ---- this thread's row of q, scaled by a power of two and rounded to fp16, into the half's operand tile
-            float factor;
+            // ---- this warp's rows of q, scaled by powers of two and rounded to fp16, into the half's operand tile.  D / 8 lanes read a row: with a row per
+            // lane the loads take a line each, 4096 of them in a CTA, and its first product waits for 5 us instead of 2.5.
+            constexpr int PIECES = D / 8, PER = 32 / PIECES;  // 16-byte pieces of a row; rows per load
+            const int piece = lane % PIECES, r0 = (warp & 3) * 32;
+            float factor = 0.0f;
             {
-                uint32_t w[D / 2];
-                uint32_t run = 0;
-                if (row < rows) {
-                    const uint4* src = reinterpret_cast<const uint4*>(a.q + ((long long)seq * a.T + token) * a.q_stride + (long long)head * D);
+                uint4 w[PIECES];
 #pragma unroll
-                    for (int i = 0; i < D / 8; ++i) {
-                        const uint4 x = __ldcg(src + i);
-                        w[4 * i] = x.x, w[4 * i + 1] = x.y, w[4 * i + 2] = x.z, w[4 * i + 3] = x.w;
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < D / 2; ++i) w[i] = 0;
+                for (int i = 0; i < PIECES; ++i) {
+                    const long long from = __shfl_sync(0xFFFFFFFFu, q_at, PER * i + lane / PIECES);
+                    w[i] = make_uint4(0u, 0u, 0u, 0u);
+                    if (from >= 0) w[i] = __ldcg(reinterpret_cast<const uint4*>(a.q + from) + piece);
                 }
 #pragma unroll
-                for (int i = 0; i < D / 2; ++i) run = __vmaxu2(run, w[i] & 0x7FFF7FFFu);
-                const int e = kv8_row_exp(max(run & 0xFFFFu, run >> 16));
-                const float up = kv8_pow2(e);
-                factor = a.scale_log2 * kv8_pow2(-e);
-                const int r = tid & 127;
+                for (int i = 0; i < PIECES; ++i) {
+                    uint32_t run = absmax_bits_bf16x8(w[i], 0u);
+                    run = max(run & 0xFFFFu, run >> 16);
 #pragma unroll
-                for (int i = 0; i < D / 8; ++i) {
-                    uint32_t x[4];
+                    for (int o = PIECES / 2; o; o >>= 1) run = max(run, __shfl_xor_sync(0xFFFFFFFFu, run, o));
+                    const int e = kv8_row_exp(run);
+                    const float up = kv8_pow2(e), down = __shfl_sync(0xFFFFFFFFu, kv8_pow2(-e), (lane % PER) * PIECES);
+                    if (lane / PER == i) factor = a.scale_log2 * down;
+                    const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+                    uint32_t y[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        x[k] = kv8_pack_half2(__uint_as_float(w[4 * i + k] << 16) * up, __uint_as_float(w[4 * i + k] & 0xFFFF0000u) * up);
-                    ptx::sts128u(base + C::Q_OFF + h * C::TILE + (i >> 3) * C::PANEL + r * 128 + (((i & 7) ^ (r & 7)) << 4), x[0], x[1], x[2], x[3]);
+                    for (int k = 0; k < 4; ++k) y[k] = kv8_pack_half2(__uint_as_float(x[k] << 16) * up, __uint_as_float(x[k] & 0xFFFF0000u) * up);
+                    const int r = r0 + PER * i + lane / PIECES;
+                    ptx::sts128u(base + C::Q_OFF + h * C::TILE + (piece >> 3) * C::PANEL + r * 128 + (((piece & 7) ^ (r & 7)) << 4), y[0], y[1], y[2], y[3]);
                 }
                 ptx::fence_proxy_async_smem();
                 __syncwarp();
@@ -273,14 +275,15 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
                     if (lane == 0) ptx::mbar_arrive(bar(C::PF + 2 * h + c));
                 }
             }
-            // ---- this thread's row of the result
+            // ---- the result: a row per thread out of tensor memory, through this warp's rows of the operand tile (no product reads it any more) to whole
+            // lines in global memory
             if (ok && n > 0) ok = ptx::warp_mbar_wait_suspend(bar(C::OF + h), 0, abort_flag);
             if (ok) {
                 ptx::tc_fence_after_sync();
                 if (ref == -INFINITY && sum == sum) sum = 0.0f;               // no key at all: what the polynomial makes of -infinity is left
                 const float inv = sum == 0.0f ? 0.0f : __fdividef(1.0f, sum);
                 const size_t part = (((size_t)unit * a.tiles + tile) * a.slices + slice) * TC_ROWS + (size_t)(row - row0);
-                uint16_t* dst = a.out + (((long long)seq * a.T + token) * a.q_heads + head) * D;
+                const uint32_t own = base + C::Q_OFF + h * C::TILE + r0 * 128;
 #pragma unroll
                 for (int c = 0; c < D; c += 32) {
                     uint32_t o[32];
@@ -291,21 +294,38 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i) o[i] = 0;
                     }
-                    if (row < rows && a.slices > 1) {
+                    if (a.slices > 1) {
+                        // 32 channels of 32 rows as they are: eight lanes write a row's 128 bytes
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4)
-                            *reinterpret_cast<uint4*>(a.part_o + part * D + c + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
-                    } else if (row < rows) {
+                        for (int i = 0; i < 8; ++i) ptx::sts128u(own + lane * 128 + ((i ^ (lane & 7)) << 4), o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                        __syncwarp();
 #pragma unroll
-                        for (int i = 0; i < 32; i += 8) {
+                        for (int i = 0; i < 8; ++i) {
+                            const int r = 4 * i + (lane >> 3);
+                            const uint4 x = ptx::lds128(own + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
+                            if (row - lane + r < rows) *reinterpret_cast<uint4*>(a.part_o + (part - lane + r) * D + c + 4 * (lane & 7)) = x;
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
                             uint32_t y[4];
 #pragma unroll
                             for (int k = 0; k < 4; ++k)
-                                y[k] = ptx::pack_bf16x2(__uint_as_float(o[i + 2 * k]) * inv, __uint_as_float(o[i + 2 * k + 1]) * inv);
-                            *reinterpret_cast<uint4*>(dst + c + i) = make_uint4(y[0], y[1], y[2], y[3]);
+                                y[k] = ptx::pack_bf16x2(__uint_as_float(o[8 * i + 2 * k]) * inv, __uint_as_float(o[8 * i + 2 * k + 1]) * inv);
+                            const int p = c / 8 + i;
+                            ptx::sts128u(own + (p >> 3) * C::PANEL + lane * 128 + (((p & 7) ^ (lane & 7)) << 4), y[0], y[1], y[2], y[3]);
                         }
                     }
-                    __syncwarp();                            // ahead of the next load of tensor memory
+                    __syncwarp();                            // ahead of the next load of tensor memory, and of the reads or writes of the operand tile
+                }
+                if (a.slices == 1) {
+#pragma unroll
+                    for (int i = 0; i < PIECES; ++i) {
+                        const int r = PER * i + lane / PIECES;
+                        const long long to = __shfl_sync(0xFFFFFFFFu, out_at, r);
+                        const uint4 x = ptx::lds128(own + (piece >> 3) * C::PANEL + r * 128 + (((piece & 7) ^ (r & 7)) << 4));
+                        if (to >= 0) *(reinterpret_cast<uint4*>(a.out + to) + piece) = x;
+                    }
                 }
                 if (a.slices > 1 && row < rows) a.part_ml[part] = make_float2(ref, sum);
             }
@@ -448,19 +468,6 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
                 for (int q = 0; q < 4; ++q) {
                     const int at = 4 * j + q, slot = at % C::SLOTS, first = (j & 3) * 8 + (q & 1) * 4;
                     if (!(ok = ptx::warp_mbar_wait_suspend(bar(C::RE + slot), ((at / C::SLOTS) & 1) ^ 1, abort_flag))) break;
-                    if (q == 0) {
-                        // The slot of the raw codes is free: the step that used it (one or two ago) is being converted, so the scores of the
-                        // second before that are complete, which follow the weights of the third: scales of five steps ago are no longer read.
-                        if ((lane >> 3) == (j & 3)) {
-                            float lg, inv;
-                            kv8_value_scale(cur.vs, lg, inv);
-                            if (cur.number < 0) lg = -INFINITY, inv = 0.0f;
-                            ptx::sts128(base + C::META_OFF + (j % TC_META) * 128 + (lane & 7) * 16,
-                                        make_float4(__half2float(__ushort_as_half((uint16_t)cur.ks)), lg, inv, 0.0f));
-                        }
-                        __syncwarp();
-                        if (lane == 0) ptx::mbar_arrive(bar(C::MF + j % TC_META));
-                    }
                     // lane i < copies: the i-th copy
                     const int number = __shfl_sync(0xFFFFFFFFu, cur.number, first + ((lane * per) >> 4 & 3));
                     const bool mine = lane < copies && number >= 0;
@@ -473,6 +480,20 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
                         ptx::bulk_g2s(base + C::RAW_OFF + slot * C::RAW + lane * per * D, src, per * D, bar(C::RF + slot));
                     }
                     __syncwarp();
+                    if (q == 0) {
+                        // After the copies, which need not wait for the scales.  The slot of the raw codes was free: the step that used it (one or two
+                        // ago) is being converted, so the scores of the second before that are complete, which follow the weights of the third: scales
+                        // of five steps ago are no longer read.
+                        if ((lane >> 3) == (j & 3)) {
+                            float lg, inv;
+                            kv8_value_scale(cur.vs, lg, inv);
+                            if (cur.number < 0) lg = -INFINITY, inv = 0.0f;
+                            ptx::sts128(base + C::META_OFF + (j % TC_META) * 128 + (lane & 7) * 16,
+                                        make_float4(__half2float(__ushort_as_half((uint16_t)cur.ks)), lg, inv, 0.0f));
+                        }
+                        __syncwarp();
+                        if (lane == 0) ptx::mbar_arrive(bar(C::MF + j % TC_META));
+                    }
                 }
             }
             if (!ok) {   // let copies already in flight land before shared memory is released
