@@ -82,25 +82,13 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
         if (lane == 0) {
             *abort_flag = 0;
             *longest_at = 0;
-            for (int i = 0; i < 2; ++i) {
-                ptx::mbar_init(bar(C::KF + i), 4);
-                ptx::mbar_init(bar(C::KE + i), 1);
-                ptx::mbar_init(bar(C::VF + i), 4);
-                ptx::mbar_init(bar(C::VE + i), 1);
-                ptx::mbar_init(bar(C::SF + i), 1);
-                ptx::mbar_init(bar(C::PF + i), 4);
-                ptx::mbar_init(bar(C::PF + 2 + i), 4);
-                ptx::mbar_init(bar(C::QF + i), 4);
-                ptx::mbar_init(bar(C::OF + i), 1);
-            }
-            for (int i = 0; i < TC_META; ++i) ptx::mbar_init(bar(C::MF + i), 1);
-            for (int i = 0; i < C::SLOTS; ++i) {
-                ptx::mbar_init(bar(C::RF + i), 1);
-                ptx::mbar_init(bar(C::RE + i), 4);
-            }
-            ptx::mbar_init(bar(C::FINAL), 1);
-            ptx::fence_mbar_init();
         }
+        // by four warps: K and V stages full, weights in place, Q in place, raw codes converted; the others by one
+        for (int i = lane; i < C::NUM_BARS; i += 32) {
+            const bool four = (i >= C::KF && i < C::KE) || (i >= C::VF && i < C::VE) || (i >= C::PF && i < C::OF) || (i >= C::RE && i < C::FINAL);
+            ptx::mbar_init(bar(i), four ? 4 : 1);
+        }
+        ptx::fence_mbar_init();
         __syncwarp();
         ptx::tmem_alloc(base + C::MISC_OFF, 512);
         ptx::tmem_relinquish();
