@@ -464,3 +464,22 @@ def test_many_blocks_of_scale_zero_with_next_to_no_weight(T):
     c.upload()
     got = c.check_attend(q, table, np.full((1, T), 120000))
     assert np.abs(got / 6e6 - 1).max() <= 2.0 ** -7
+
+
+@pytest.mark.parametrize("B_,T,heads,rep,dim,block,keys", [(1, 1024, 8, 4, 128, 64, 1400), (2, 400, 10, 4, 64, 16, 1500), (90, 33, 1, 1, 64, 32, 1300)])
+@pytest.mark.parametrize("shape", ["even", "rising", "one long", "none"])
+def test_attention_where_some_tiles_are_long(B_, T, heads, rep, dim, block, keys, shape):
+    """Nearly as many row tiles as SMs, of equal and of very different lengths, rows without a key among them."""
+    _, c, table, q = attend_case(B_ + T, B_, T, heads, rep, dim, block, keys)
+    limits = np.full((B_, T), keys)
+    if shape == "rising":
+        limits = (keys * (np.arange(B_ * T) + 1) // (B_ * T)).reshape(B_, T)
+        limits[0, :5] = 0
+    elif shape != "even":
+        limits[:] = 0 if shape == "none" else 100
+        limits[B_ // 2, T // 2] = 0 if shape == "none" else keys
+        limits[B_ - 1, 3] = 0
+    got = c.check_attend(q, table, limits)
+    assert (got[limits == 0] == 0).all()
+    again = c.attend(q, table, limits, dim ** -0.5)
+    assert torch.equal(again, c.attend(q, table, limits, dim ** -0.5))
