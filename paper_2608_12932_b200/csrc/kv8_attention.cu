@@ -88,29 +88,21 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     const int rows = a.T * a.rep;
     ptx::pdl_wait();
 
-    // ---- this lane's rows' limits; and q as fp16 operand, with the factors that undo its powers of two, through shared memory: eight rows (half a
-    // block of 16) from each of the first 2 RB warps
+    // ---- this lane's rows' limits (all loads ahead of the first use); and q: eight rows (half a block of 16) in each of the first 2 RB warps, in flight
+    // while the first copies are issued, then as fp16 operand, with the factors that undo its powers of two, through shared memory
     int limit[RB][2];
     int longest = 0, shortest = 0x7FFFFFFF;
     const int capacity = (int)min((long long)a.table_width << a.log2_block, 0x7FFFFF00ll);
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = rb * 16 + h * 8 + g;
-            limit[rb][h] = 0;
-            if (r < rows) {
-                limit[rb][h] = min(max(__ldcg(a.limits + (long long)seq * a.T + r / a.rep), 0), capacity);
-                shortest = min(shortest, limit[rb][h]);
-            }
-            longest = max(longest, limit[rb][h]);
-        }
+        for (int h = 0; h < 2; ++h) limit[rb][h] = __ldcg(a.limits + (long long)seq * a.T + min(rb * 16 + h * 8 + g, rows - 1) / a.rep);
     }
-    if (warp < 2 * RB) {
-        const int rb = warp >> 1, h = warp & 1, r = rb * 16 + h * 8 + g;
-        uint32_t w[KS * 2];
+    uint32_t w[KS * 2];
 #pragma unroll
-        for (int i = 0; i < KS * 2; ++i) w[i] = 0;
+    for (int i = 0; i < KS * 2; ++i) w[i] = 0;
+    if (warp < 2 * RB) {
+        const int r = (warp >> 1) * 16 + (warp & 1) * 8 + g;
         if (r < rows) {
             const int token = r / a.rep, head = kv_head * a.rep + r - token * a.rep;
             const uint16_t* src = a.q + ((long long)seq * a.T + token) * a.q_stride + (long long)head * D + 16 * t;
@@ -121,21 +113,15 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
                 w[8 * i + 4] = y.x, w[8 * i + 5] = y.y, w[8 * i + 6] = y.z, w[8 * i + 7] = y.w;
             }
         }
-        uint32_t run = 0;
+    }
 #pragma unroll
-        for (int i = 0; i < KS * 2; ++i) run = __vmaxu2(run, w[i] & 0x7FFF7FFFu);
-        run = max(run & 0xFFFFu, run >> 16);
-        run = max(run, __shfl_xor_sync(0xFFFFFFFFu, run, 1));
-        run = max(run, __shfl_xor_sync(0xFFFFFFFFu, run, 2));
-        const int e = kv8_row_exp(run);
-        const float up = kv8_pow2(e);
-        if (t == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(smem + C::FACTOR_OFF + (rb * 16 + h * 8 + g) * 4), "f"(a.scale_log2 * kv8_pow2(-e)) : "memory");
+    for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
-        for (int i = 0; i < KS; ++i) {
-            // words h and 2 + h of the lane's four
-            const uint32_t at = smem + C::Q_OFF + ((i * RB + rb) * 32 + lane) * 16 + 4 * h;
-            asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(kv8_pack_half2(__uint_as_float(w[2 * i] << 16) * up, __uint_as_float(w[2 * i] & 0xFFFF0000u) * up)) : "memory");
-            asm volatile("st.shared.u32 [%0], %1;" ::"r"(at + 8), "r"(kv8_pack_half2(__uint_as_float(w[2 * i + 1] << 16) * up, __uint_as_float(w[2 * i + 1] & 0xFFFF0000u) * up)) : "memory");
+        for (int h = 0; h < 2; ++h) {
+            const bool real = rb * 16 + h * 8 + g < rows;
+            limit[rb][h] = real ? min(max(limit[rb][h], 0), capacity) : 0;
+            shortest = min(shortest, real ? limit[rb][h] : 0x7FFFFFFF);
+            longest = max(longest, limit[rb][h]);
         }
     }
     longest = __reduce_max_sync(0xFFFFFFFFu, longest);
@@ -150,23 +136,24 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     const int chunk_shift = a.log2_block - 4;                // chunks per block, as a shift
     const int32_t* table = a.table + (size_t)seq * a.table_width;
     // lane j holds block number and scales of this warp's chunk of turn 32 i + j, for the current 32 turns and the next
-    struct Meta { int number; uint32_t scales; };            // scales: key's, value's
+    struct Meta { int number; uint32_t ks, vs; };
     auto meta_of = [&](int base) -> Meta {
-        Meta m = {-1, 0u};
+        Meta m = {-1, 0u, 0u};
         const int c = first + 4 * (base + lane);
         if (base + lane < turns && c < c_hi) {
             const int number = __ldcg(table + (c >> chunk_shift));
             if ((unsigned)number < (unsigned)a.num_blocks) {
                 const size_t at = (size_t)number * a.kv_heads + kv_head;
                 m.number = number;
-                m.scales = (uint32_t)__ldcg(a.k_scales + at) | (uint32_t)__ldcg(a.v_scales + at) << 16;
+                m.ks = __ldcg(a.k_scales + at);
+                m.vs = __ldcg(a.v_scales + at);
             } else {
                 *a.status = W4A8_ERR_INDEX;                  // positions of a block that does not exist count as not there
             }
         }
         return m;
     };
-    Meta cur = meta_of(0), nxt = {-1, 0u};
+    Meta cur = meta_of(0), nxt = {-1, 0u, 0u};
     if (turns > 32) nxt = meta_of(32);
     int base = 0;
     const uint32_t ring = smem + warp * (C::STAGES * C::STAGE), other_ring = smem + (warp ^ 1) * (C::STAGES * C::STAGE);
@@ -193,6 +180,25 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     };
 #pragma unroll
     for (int i = 0; i < C::STAGES - 1; ++i) issue(i);
+    if (warp < 2 * RB) {                                     // (the first copies are on their way)
+        const int rb = warp >> 1, h = warp & 1;
+        uint32_t run = 0;
+#pragma unroll
+        for (int i = 0; i < KS * 2; ++i) run = __vmaxu2(run, w[i] & 0x7FFF7FFFu);
+        run = max(run & 0xFFFFu, run >> 16);
+        run = max(run, __shfl_xor_sync(0xFFFFFFFFu, run, 1));
+        run = max(run, __shfl_xor_sync(0xFFFFFFFFu, run, 2));
+        const int e = kv8_row_exp(run);
+        const float up = kv8_pow2(e);
+        if (t == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(smem + C::FACTOR_OFF + (rb * 16 + h * 8 + g) * 4), "f"(a.scale_log2 * kv8_pow2(-e)) : "memory");
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            // words h and 2 + h of the lane's four
+            const uint32_t at = smem + C::Q_OFF + ((i * RB + rb) * 32 + lane) * 16 + 4 * h;
+            asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(kv8_pack_half2(__uint_as_float(w[2 * i] << 16) * up, __uint_as_float(w[2 * i] & 0xFFFF0000u) * up)) : "memory");
+            asm volatile("st.shared.u32 [%0], %1;" ::"r"(at + 8), "r"(kv8_pack_half2(__uint_as_float(w[2 * i + 1] << 16) * up, __uint_as_float(w[2 * i + 1] & 0xFFFF0000u) * up)) : "memory");
+        }
+    }
     __syncthreads();                                         // q and flags are there
     float factor[RB][2];
     uint32_t qf[RB == 1 ? KS : 1][4];                        // 16 rows: q stays in registers
@@ -230,7 +236,7 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
         cp_async_wait<C::STAGES - 2>();
         __syncwarp();
         const int number = __shfl_sync(0xFFFFFFFFu, cur.number, i & 31);
-        const uint32_t scales = __shfl_sync(0xFFFFFFFFu, cur.scales, i & 31);
+        const uint32_t scales = __shfl_sync(0xFFFFFFFFu, cur.ks | cur.vs << 16, i & 31);         // (put together here: copies do not wait for them)
         const int key0 = (first + 4 * i) * AR_CHUNK;
         const uint32_t kst = ring + slot * C::STAGE + k_at;
         // ---- scores of this warp's 16 positions: columns 8 n + 2 t, + 1
