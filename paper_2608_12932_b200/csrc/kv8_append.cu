@@ -7,8 +7,8 @@
 // d the scales' distance in octaves, against half an fp32 step of at most 2^-(17+d)): the codes are those of exact arithmetic.
 //
 // One CTA per (sequence, touched block, head) and for K and V apart: it owns all that it reads and writes of the cache.
-// HBM-bound for a chunk of new tokens (2 B in, 1 B out per element); for single tokens a latency chain (position, table,
-// scale, new values, store).
+// For single tokens a latency chain (position, new values and table, scale, reduction, store): 2.0 us a launch in a chain.  A chunk moves 2 B in and 1 B
+// out per element, but is over before the chain has paid for itself: 1391 tokens of 8 heads x 128 in blocks of 128 5.3 us, 1.6 TB/s.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include "ptx_sm100.cuh"
@@ -162,6 +162,7 @@ cudaError_t launch_kv8_append(const w4a8_kv8_cache& c, const void* k, const void
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     const int most = (T < c.block ? T : c.block) * a.pieces;                     // pieces of new values in one block
+    // (128 threads for large blocks: 5.6 instead of 5.3 us above; 512 for few new tokens: 40 of them 3.2 instead of 2.0)
     const int threads = most > 2 * APPEND_FEW ? APPEND_MANY : APPEND_FEW;
     const int per = (most + threads - 1) / threads;
     cfg.blockDim = dim3((unsigned)threads, 1, 1);

@@ -6,7 +6,9 @@
 // each pair with its own running sums: a warp fetches 16 positions' codes (16-byte asynchronous copies into a ring of its own), forms their
 // scores and weights, hands the weights to its partner through shared memory, and multiplies the values of all 32 positions for its half of the
 // channels.  So a warp keeps half a tile's sums: a warp that keeps all of them needs 255 registers at 32 rows, and two warps
-// per scheduler leave it idle most of the time (a draft block of 8 over 32749 positions: 39 us).
+// per scheduler leave it idle most of the time (a draft block of 8 over 32749 positions: 39 us).  Bound by instruction issue, not by the cache's
+// bytes: that block 27.4 us (2.4 TB/s; conversion, addresses and weights are 520 warp instructions per 16 positions), one token over
+// 65000 positions 31.5 us (4.2 TB/s); a single short sequence by the chain of limits, table, codes, and by the second launch (4096 positions 8.4 us).
 // mma.m16n8k16 with the rows on the 16-row side.  The order of the contraction index is free as long as both operands
 // agree, and so is the order of the output channels, so a lane takes 16 neighbouring codes of a key for the first product and neighbouring
 // channels of four values for the second, and converts them in registers: nothing is transposed through shared memory.  The
@@ -478,7 +480,8 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
 
 // W warps per (token, head) row, each with its share of the slices: sums weighted by how far their reference is below the largest.  With four
 // warps per row one decode token's 32 slices take one round of loads (one warp per row took most of 6 us); up to eight slices, and so with many
-// rows, one warp has them under way at once (four: 200 rows of 28 heads 38.7 instead of 29 us altogether).
+// rows, one warp has them under way at once.  Attention altogether, one or four warps a row: 32 slices 10.6 and 8.4 us, 18 slices 34.3 and 27.4;
+// 6 slices of 200 tokens x 28 heads 24.4 and 33.8.
 template <int D, int W>
 __global__ void __launch_bounds__(128)
 kv8_combine_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, uint16_t* __restrict__ out, long long total_rows, int T,
@@ -614,6 +617,8 @@ cudaError_t launch_combine(const AttendArgs& a, int B, int tile_rows, cudaStream
 }  // namespace
 
 // Row tiles of 16 with four CTAs per SM, of 32 with three, of 256 with one: what is resident at once.
+// Measured (8 key heads of 128, 1000, 4096 and 32749 positions): 16 rows 6.3, 9.7, 25.2 us as tiles of 16; 7.6, 11.3, 26.6 as tiles of 32; 10.8, 13.5, 40.1
+// as tiles of 256.  32 rows 8.2, 12.1, 27.6 as tiles of 32; 10.9, 13.4, 40.3 as tiles of 256, which take no longer for 64 rows (10.7, 13.5, 40.5).
 static int ctas_per_sm(int rows) { return rows == 16 ? ArCfg<128, 1>::CTAS : (rows == 32 ? ArCfg<128, 2>::CTAS : 1); }
 
 Kv8Plan kv8_plan(int B, int T, int q_heads, int kv_heads, long long max_keys, int sms) {
@@ -623,7 +628,8 @@ Kv8Plan kv8_plan(int B, int T, int q_heads, int kv_heads, long long max_keys, in
     p.tiles = (int)((rows + p.rows - 1) / p.rows);
     const long long units = (long long)B * kv_heads * p.tiles;
     long long s = (long long)ctas_per_sm(p.rows) * sms / units;
-    // two chunks for each of a CTA's warps, two steps of the tensor-memory kernel
+    // at least two chunks for each of a CTA's warps, two steps of the tensor-memory kernel (with four of those a chunk of 200 tokens over 2900
+    // positions takes 35.6 instead of 30.8 us, and equally long with a bound of 512; 100 tokens over 1000 24.8 instead of 21.7)
     const long long most = p.rows == 256 ? (max_keys + 255) / 256 : (max_keys + 127) / 128;
     if (s > most) s = most;
     p.slices = (int)(s < 1 ? 1 : s);

@@ -10,7 +10,8 @@
 // the maximum that the scale needs travel through one block reduction instead of two, and the codes are still exactly those
 // of the quantiser on h.  The sum of squares is fp32 (per thread, then a tree); the one rounding of h to bf16 is the
 // quantiser's input format, as after SiLU * up.
-// HBM-bound for many rows (7 B per element with a residual, 3 without); for few rows a latency chain of load, reduction, store.
+// HBM-bound for many rows (7 B per element with a residual, 3 without): 4096 rows of 5120 with a residual 31 us, 4.7 TB/s, CTAs whose loads
+// and stores follow one another; for few rows a latency chain of load, reduction, store (one row of 4096: 2.4 us a launch in a chain).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include "ptx_sm100.cuh"
@@ -40,9 +41,9 @@ __device__ __forceinline__ uint32_t norm2(uint32_t s, uint32_t w, float rstd) {
 }
 
 // T threads per row, CACHE chunks of 8 elements per thread in registers (a longer row's rest is read again: from sum_out, which
-// may have overwritten x or r).  FAST: the quantiser's reciprocal form (see quantize_act.cu), for many rows.
-template <int T, int CACHE, bool FAST, bool ADD>
-__global__ void __launch_bounds__(T, FAST && T == 256 ? (CACHE <= 3 ? 5 : 3) : 1)
+// may have overwritten x or r).  Codes by the quantiser's reciprocal form (see quantize_act.cu).
+template <int T, int CACHE, bool ADD>
+__global__ void __launch_bounds__(T, T == 256 ? (CACHE <= 3 ? 5 : 3) : 1)
 add_rmsnorm_quantize_kernel(const uint4* x, const uint4* r, const uint4* __restrict__ w, float eps, int K, uint4* sum_out, uint4* h_out,
                             uint2* __restrict__ qa, uint16_t* __restrict__ sa, int32_t* __restrict__ asum) {
     ptx::pdl_launch_dependents();
@@ -104,7 +105,7 @@ add_rmsnorm_quantize_kernel(const uint4* x, const uint4* r, const uint4* __restr
     const __half sh = row_scale_from_amax_bits(amax);
     const float s = __half2float(sh);
     if (tid == 0) sa[m] = __half_as_ushort(sh);
-    const bool fast_row = FAST && __half_as_ushort(sh) < 0x7BFFu;
+    const bool fast_row = __half_as_ushort(sh) < 0x7BFFu;
     const float rinv = s != 0.0f ? __frcp_rn(s) : 0.0f;
 
     // sixteen neighbouring chunks are one group of 128 and sit in the 16 lanes of one half-warp (see quantize_act_kernel)
@@ -140,12 +141,12 @@ add_rmsnorm_quantize_kernel(const uint4* x, const uint4* r, const uint4* __restr
     for (int c = tid + CACHE * T; c < chunks; c += T) emit(c, __ldcg((ADD ? sum_out : x) + row + c));
 }
 
-template <int T, int CACHE, bool FAST>
+template <int T, int CACHE>
 cudaError_t launch_norm(cudaLaunchConfig_t cfg, const uint4* x, const uint4* r, const uint4* w, float eps, int K, uint4* sum, uint4* h,
                         uint2* qa, uint16_t* sa, int32_t* asum) {
     cfg.blockDim = dim3(T, 1, 1);
-    if (r) return cudaLaunchKernelEx(&cfg, add_rmsnorm_quantize_kernel<T, CACHE, FAST, true>, x, r, w, eps, K, sum, h, qa, sa, asum);
-    return cudaLaunchKernelEx(&cfg, add_rmsnorm_quantize_kernel<T, CACHE, FAST, false>, x, r, w, eps, K, sum, h, qa, sa, asum);
+    if (r) return cudaLaunchKernelEx(&cfg, add_rmsnorm_quantize_kernel<T, CACHE, true>, x, r, w, eps, K, sum, h, qa, sa, asum);
+    return cudaLaunchKernelEx(&cfg, add_rmsnorm_quantize_kernel<T, CACHE, false>, x, r, w, eps, K, sum, h, qa, sa, asum);
 }
 
 }  // namespace
@@ -163,15 +164,15 @@ cudaError_t launch_add_rmsnorm_quantize(const void* x, const void* residual, con
     const uint4 *xp = static_cast<const uint4*>(x), *rp = static_cast<const uint4*>(residual), *wp = static_cast<const uint4*>(weight);
     uint4 *sp = static_cast<uint4*>(sum_out), *hp = static_cast<uint4*>(h_out);
     uint2* qp = reinterpret_cast<uint2*>(qa);
-    if (K <= 1024) return launch_norm<128, 1, false>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
-    if (M <= 512) {
-        if (K <= 2048) return launch_norm<256, 1, false>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
-        if (K <= 4096) return launch_norm<512, 1, false>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
-        return launch_norm<512, 3, false>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
-    }
-    if (K <= 4096) return launch_norm<256, 2, true>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
-    if (K <= 6144) return launch_norm<256, 3, true>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
-    return launch_norm<256, 6, true>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
+    // Threads per row by the row's length, so that it fits their registers.  Up to 256 rows twice as many threads where 256 would hold more than one chunk of a
+    // short row or three of a long one (200 rows of 4096: 3.7 against 4.4 us, of 8192 5.6 against 6.3; from 500 rows on the wider CTAs are slower,
+    // 500 of 4096 6.6 against 6.0, 4096 of 5120 53 against 31).  Rows of 1024 with 256 threads: 4096 of them 12.5 instead of 8.5 us.
+    if (K <= 1024) return launch_norm<128, 1>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
+    if (M <= 256 && K > 2048 && K <= 4096) return launch_norm<512, 1>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
+    if (M <= 256 && K > 6144) return launch_norm<512, 3>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
+    if (K <= 4096) return launch_norm<256, 2>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
+    if (K <= 6144) return launch_norm<256, 3>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
+    return launch_norm<256, 6>(cfg, xp, rp, wp, eps, K, sp, hp, qp, sa, asum);
 }
 
 }  // namespace w4a8
