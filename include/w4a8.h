@@ -281,7 +281,7 @@ w4a8_status w4a8_add_rmsnorm_quantize(const void* x_bf16, const void* residual_b
  * values of a window of frames, Sec. 3.1; it names no format for them, this is the one of the activations, per block).
  *
  *   k_codes, v_codes    int8 [num_blocks][heads][block][dim], 16-byte aligned; a key or value is its code times the scale of
- *   k_scales, v_scales  fp16 [num_blocks][heads], not negative          its block and head
+ *   k_scales, v_scales  fp16 [num_blocks][heads], finite, not negative  its block and head
  *   block 16, 32, 64 or 128 tokens;  dim 64 or 128;  heads = key/value heads
  * A sequence is a list of blocks: table int32 [B][table_width], entry i the number of the block that holds positions
  * i block .. i block + block - 1.  Several sequences may read one block.  Entries past a sequence's last position are not read.
@@ -311,7 +311,8 @@ typedef struct {
  *   start     device, int32 [B];  count  device, int32 [B] (values outside 0 .. T count as the nearest), or NULL: T each
  *   workspace at least W4A8_WORKSPACE_HEADER_BYTES, initialised (w4a8_workspace_init): its status word
  * The blocks that one call writes must be distinct, and not written by another call at the same time.
- * Run again on the same input it changes nothing.  B, 2 heads <= 65535.
+ * Run again on the same input it changes nothing.  Not-a-number or infinity among the new values: codes and scale of that block
+ * and head are undefined, as for w4a8_quantize_act.  B, 2 heads <= 65535.
  */
 w4a8_status w4a8_kv8_append(const w4a8_kv8_cache* cache, const void* k_bf16, const void* v_bf16, long long k_stride,
                             long long v_stride, int B, int T, const int32_t* table, int table_width, const int32_t* start,
@@ -329,7 +330,7 @@ w4a8_status w4a8_kv8_append(const w4a8_kv8_cache* cache, const void* k_bf16, con
  * fp64 definition.  A row of q with an infinity or not-a-number gives not-a-number in that row alone.
  *   q         device, bf16, 16-byte aligned: row b T + t holds q_heads x dim contiguous values, rows q_stride elements apart
  *             (a multiple of 8, at least q_heads dim)
- *   limits    device, int32 [B][T];  out  device, bf16 [B T][q_heads dim], 16-byte aligned
+ *   limits    device, int32 [B][T];  out  device, bf16 [B T][q_heads dim], 16-byte aligned, not overlapping q
  *   workspace at least w4a8_kv8_workspace_bytes(dim) bytes, 256-byte aligned, initialised once; the same rules as for
  *             w4a8_gemm, with whose calls it may be shared on one stream.  Enough for any call of this dim; 0: unsupported dim
  * Up to 32 rows (tokens x query heads of a group) the cache streams through the kernel for few rows, above through the tcgen05
