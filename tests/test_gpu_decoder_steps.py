@@ -483,3 +483,36 @@ def test_attention_where_some_tiles_are_long(B_, T, heads, rep, dim, block, keys
     assert (got[limits == 0] == 0).all()
     again = c.attend(q, table, limits, dim ** -0.5)
     assert torch.equal(again, c.attend(q, table, limits, dim ** -0.5))
+
+
+@pytest.mark.parametrize("T", [1, 8, 150])
+def test_blocks_that_are_shared(T):
+    """Sequences with a common prefix, and one that names a block twice."""
+    _, c, table, q = attend_case(T + 40, 3, T, 2, 4, 64, 16, 400)
+    table[1, :7] = table[0, :7]
+    table[2, 9] = table[2, 3]
+    c.check_attend(q, table, causal([400, 333, 390], T))
+
+
+def test_two_graphs_on_one_workspace():
+    """Captured calls of different kernels that share a workspace, replayed in turn."""
+    cases = []
+    for T, keys in ((1, 3000), (150, 900)):
+        _, c, table, q = attend_case(T + 41, 1, T, 2, 4, 128, 64, keys)
+        cases.append((c, i32(table), t_u16(q[0], torch.bfloat16), i32(causal([keys], T)), torch.empty((T, 1024), dtype=torch.bfloat16, device="cuda")))
+    ws = cases[0][0].ws
+    want = [B.w4a8_kv8_attention(q, c.dev, t, l, 0.1, ws) for c, t, q, l, _ in cases]
+    torch.cuda.synchronize()
+    graphs = []
+    for c, t, q, l, out in cases:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            B.w4a8_kv8_attention(q, c.dev, t, l, 0.1, ws, out=out)
+        graphs.append(g)
+    for i in (0, 1, 0, 0, 1, 1, 0):
+        cases[i][-1].zero_()
+        graphs[i].replay()
+        graphs[1 - i].replay()
+        torch.cuda.synchronize()
+        for (*_, out), w in zip(cases, want):
+            assert torch.equal(out, w)
