@@ -628,7 +628,8 @@ Kv8Plan kv8_plan(int B, int T, int q_heads, int kv_heads, long long max_keys, in
     p.tiles = (int)((rows + p.rows - 1) / p.rows);
     const long long units = (long long)B * kv_heads * p.tiles;
     long long s = (long long)ctas_per_sm(p.rows) * sms / units;
-    // at least two chunks for each of a CTA's warps, two steps of the tensor-memory kernel (with four of those a chunk of 200 tokens over 2900
+    // at least two chunks for each of a CTA's warps (with one, or four: one token over 500 positions 5.0 and 6.7 instead of 5.5 us, over 4096 8.7 and 8.9
+    // instead of 8.5; a draft block of 8 over 4096 13.4 and 13.8 instead of 12.2), two steps of the tensor-memory kernel (with four of those a chunk of 200 tokens over 2900
     // positions takes 35.6 instead of 30.8 us, and equally long with a bound of 512; 100 tokens over 1000 24.8 instead of 21.7)
     const long long most = p.rows == 256 ? (max_keys + 255) / 256 : (max_keys + 127) / 128;
     if (s > most) s = most;
