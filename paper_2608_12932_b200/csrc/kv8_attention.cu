@@ -6,9 +6,9 @@
 // each pair with its own running sums: a warp fetches 16 positions' codes (16-byte asynchronous copies into a ring of its own), forms their
 // scores and weights, hands the weights to its partner through shared memory, and multiplies the values of all 32 positions for its half of the
 // channels.  So a warp keeps half a tile's sums: a warp that keeps all of them needs 255 registers at 32 rows, and two warps
-// per scheduler leave it idle most of the time (a draft block of 8 over 32749 positions: 39 us).  Bound by instruction issue, not by the cache's
-// bytes: that block 27.4 us (2.4 TB/s; conversion, addresses and weights are 520 warp instructions per 16 positions), one token over
-// 65000 positions 31.5 us (4.2 TB/s); a single short sequence by the chain of limits, table, codes, and by the second launch (4096 positions 8.4 us).
+// per scheduler leave it idle most of the time (a draft block of 8 over 32749 positions: 39 us).  Bound by a chunk's chain of dependent steps and its
+// 520 warp instructions per 16 positions, not by the cache's bytes: that block 27.4 us (2.4 TB/s, issue 0.48 a cycle and scheduler), one token over
+// 65000 positions 31.5 us (4.2 TB/s, 0.59); a single short sequence by the chain of limits, table, codes, and by the second launch (4096 positions 8.4 us).
 // mma.m16n8k16 with the rows on the 16-row side.  The order of the contraction index is free as long as both operands
 // agree, and so is the order of the output channels, so a lane takes 16 neighbouring codes of a key for the first product and neighbouring
 // channels of four values for the second, and converts them in registers: nothing is transposed through shared memory.  The

@@ -516,3 +516,24 @@ def test_two_graphs_on_one_workspace():
         torch.cuda.synchronize()
         for (*_, out), w in zip(cases, want):
             assert torch.equal(out, w)
+
+
+@pytest.mark.parametrize("T,B_", [(1, 1), (3, 5), (8, 2), (37, 3), (150, 1), (300, 2)])
+def test_rows_behind_the_last_are_left_as_they_are(T, B_):
+    """Outputs in the middle of larger buffers, not-a-number in front of and behind q's rows."""
+    _, c, table, q = attend_case(T + 60, B_, T, 2, 3, 64, 16, 310)
+    limits = causal([310 - 7 * b for b in range(B_)], T)
+    M = B_ * T
+    big = torch.full((M + 40, 6 * 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    qb = torch.full((M + 40, 6, 64), float("nan"), dtype=torch.bfloat16, device="cuda")
+    qb[20:20 + M] = t_u16(q.reshape(M, 6, 64), torch.bfloat16)
+    B.w4a8_kv8_attention(qb[20:20 + M], c.dev, i32(table), i32(limits), 0.1, c.ws, out=big[20:20 + M])
+    torch.cuda.synchronize()
+    assert torch.equal(big[20:20 + M], c.attend(q, table, limits, 0.1))
+    assert (big[:20] == 7).all() and (big[20 + M:] == 7).all()
+    x, r, w = norm_case(M, 640, T)
+    outs = [torch.full((M + 2, n), 5, dtype=t, device="cuda") for n, t in ((640, torch.bfloat16), (640, torch.int8), (1, torch.float16), (5, torch.int32))]
+    s, qa, sa, asum = (o[1:1 + M] for o in outs)
+    B.w4a8_add_rmsnorm_quantize(t_u16(x, torch.bfloat16), t_u16(w, torch.bfloat16), 1e-6, residual=t_u16(r, torch.bfloat16), sum_out=s, out=(qa, sa.view(-1), asum))
+    torch.cuda.synchronize()
+    assert all((o[0] == 5).all() and (o[-1] == 5).all() for o in outs)
