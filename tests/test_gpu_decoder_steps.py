@@ -537,3 +537,25 @@ def test_rows_behind_the_last_are_left_as_they_are(T, B_):
     B.w4a8_add_rmsnorm_quantize(t_u16(x, torch.bfloat16), t_u16(w, torch.bfloat16), 1e-6, residual=t_u16(r, torch.bfloat16), sum_out=s, out=(qa, sa.view(-1), asum))
     torch.cuda.synchronize()
     assert all((o[0] == 5).all() and (o[-1] == 5).all() for o in outs)
+
+
+def test_many_sequences():
+    """The largest grids: 65528 (sequence, head) pairs that all read the same blocks, for single tokens, draft blocks and more rows; as many appends."""
+    n, heads = 8191, 8
+    _, c, table, q = attend_case(70, 1, 40, heads, 1, 64, 16, 50)
+    wide = torch.from_numpy(np.repeat(table, n, axis=0).astype(np.int32)).cuda()
+    for T in (1, 20, 40):
+        limits = causal([50], T)
+        want = c.attend(q[:, :T], table, limits, 0.1)
+        got = B.w4a8_kv8_attention(t_u16(q[0, :T], torch.bfloat16).repeat(n, 1, 1), c.dev, wide, i32(np.repeat(limits, n, axis=0)), 0.1, c.ws)
+        torch.cuda.synchronize()
+        assert (got.view(n, T, -1) == want).all()
+    rng = np.random.default_rng(71)
+    k, v = new_values(rng, 1, 3, heads, 64)
+    one, many = Cache(rng, 1, heads, 16, 64), B.KV8Cache.empty(n, heads, 64, 16)
+    one.append(k, v, np.array([[0]]), [0])
+    B.w4a8_kv8_append(many, t_u16(k[0], torch.bfloat16).repeat(n, 1, 1), t_u16(v[0], torch.bfloat16).repeat(n, 1, 1),
+                      torch.arange(n, dtype=torch.int32, device="cuda")[:, None].contiguous(), torch.zeros(n, dtype=torch.int32, device="cuda"), one.ws)
+    torch.cuda.synchronize()
+    assert (many.k_codes[:, :, :3] == one.dev.k_codes[:, :, :3]).all() and (many.v_codes[:, :, :3] == one.dev.v_codes[:, :, :3]).all()
+    assert (many.k_scales == one.dev.k_scales).all() and (many.v_scales == one.dev.v_scales).all()
