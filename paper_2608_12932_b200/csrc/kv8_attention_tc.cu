@@ -45,29 +45,6 @@ struct TcCfg {
     static constexpr uint32_t S_COL = 0, O_COL = 256;                            // tensor memory: scores 2 x 128 columns, sums 2 x 128
 };
 
-constexpr int TC_POLY = 2;                                    // of eight pairs of exponentials, those taken by the polynomial
-// 2^x and 2^y without the special-function unit: x = n + f with n the nearest integer (which lands in the low mantissa bits of x + 1.5 2^23), 2^f
-// on [-1/2, 1/2] by the polynomial of degree 4 with the smallest largest relative error, 2.6e-6 (Remez), n added to the exponent.
-// Below -126, and for not-a-number, a denormal number of nearly 2^-126: nothing as an fp16 weight, nothing in a sum that has a reference (and a row
-// that is not a number has its other weights to say so).
-__device__ __forceinline__ float2 exp2_poly2(float x, float y) {
-    constexpr float C4 = 0.009570102207362652f, C3 = 0.05591785907745361f, C2 = 0.240247443318367f, C1 = 0.6931217908859253f, C0 = 0.9999992847442627f;
-    constexpr float MAGIC = 12582912.0f;
-    auto both = [](float v) { return ptx::pack2(__float_as_uint(v), __float_as_uint(v)); };
-    x = fmaxf(x, -126.0f);
-    y = fmaxf(y, -126.0f);
-    const uint64_t v = ptx::pack2(__float_as_uint(x), __float_as_uint(y));
-    const uint64_t t = ptx::add2(v, both(MAGIC));
-    const uint64_t n = ptx::add2(t, both(-MAGIC));
-    const uint64_t f = ptx::fma2(n, both(-1.0f), v);
-    uint64_t p = ptx::fma2(f, both(C4), both(C3));
-    p = ptx::fma2(p, f, both(C2));
-    p = ptx::fma2(p, f, both(C1));
-    p = ptx::fma2(p, f, both(C0));
-    const float2 r = ptx::unpack2(p), e = ptx::unpack2(t);
-    return make_float2(__uint_as_float(__float_as_uint(r.x) + (__float_as_uint(e.x) << 23)), __uint_as_float(__float_as_uint(r.y) + (__float_as_uint(e.y) << 23)));
-}
-
 template <int D>
 __global__ void __launch_bounds__(TC_THREADS, 1)
 kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
@@ -237,7 +214,8 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
                         }
                     }
                 }
-                // ---- the weights, handed over 64 positions at a time.  Some exponentials are taken by the polynomial, on the FMA pipe.
+                // ---- the weights, handed over 64 positions at a time (a quarter of the exponentials by a polynomial on the FMA pipe: 147 -> 156 us for the
+                // prompt; the special-function unit is not what the warps wait for)
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     uint32_t p[32];
@@ -248,11 +226,7 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
                         for (int i = 0; i < 8; ++i) {
                             const int at = (4 * c + b) * 16 + 2 * i;
                             const float x = __uint_as_float(s[at >> 5][at & 31]), y = __uint_as_float(s[at >> 5][(at & 31) + 1]);
-                            float2 w;
-                            if (i < TC_POLY)
-                                w = exp2_poly2(x, y);
-                            else
-                                w = make_float2(kv8_ex2(x), kv8_ex2(y));
+                            const float2 w = make_float2(kv8_ex2(x), kv8_ex2(y));
                             g = ptx::add2(g, ptx::pack2(__float_as_uint(w.x), __float_as_uint(w.y)));
                             p[b * 8 + i] = kv8_pack_half2(w.x, w.y);
                         }
@@ -271,7 +245,6 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
             if (ok && n > 0) ok = ptx::warp_mbar_wait_suspend(bar(C::OF + h), 0, abort_flag);
             if (ok) {
                 ptx::tc_fence_after_sync();
-                if (ref == -INFINITY && sum == sum) sum = 0.0f;               // no key at all: what the polynomial makes of -infinity is left
                 const float inv = sum == 0.0f ? 0.0f : __fdividef(1.0f, sum);
                 const size_t part = (((size_t)unit * a.tiles + tile) * a.slices + slice) * TC_ROWS + (size_t)(row - row0);
                 const uint32_t own = base + C::Q_OFF + h * C::TILE + r0 * 128;
