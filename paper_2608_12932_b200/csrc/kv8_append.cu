@@ -107,7 +107,7 @@ kv8_append_kernel(const AppendArgs a) {
         }
     }
     if (tid == 0) *scale = (uint16_t)bits;
-    const bool fast = bits < 0x7BFFu;
+    const bool fast = fast_scale(bits);
     const float rinv = s != 0.0f ? __frcp_rn(s) : 0.0f;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {

@@ -44,9 +44,17 @@ __device__ __forceinline__ uint2 quant8(const uint4& v, float s, int& sum) {
     return o;
 }
 
+// The scales (fp16 bits) for which codes may be formed by the reciprocal, which has no clamp and so needs |x / s| < 127.5 - 2^-13 (products are
+// within 2^-16 of their quotients).  From 2^-14 on s is amax / 127 but for a factor of 1 +- 2^-11: |x / s| < 127.1.  Below, s = n 2^-24 with amax / 127 at most
+// (n + 1/2) 2^-24: |x / s| <= 127 + 63.5 / n, which is 127.4961 for n = 128 and more from there down to 190.5 for n = 1.  At the other end a scale
+// that saturated at 65504 bounds nothing.  A scale taken from older values as well (the append's) is larger, its quotients smaller.
+constexpr uint32_t FAST_SCALE_FIRST = 0x0080u, FAST_SCALE_END = 0x7BFFu;
+__device__ __forceinline__ bool fast_scale(uint32_t fp16_bits) {
+    return fp16_bits >= FAST_SCALE_FIRST && fp16_bits < FAST_SCALE_END;
+}
+
 // Fast path of a chunk (see quantize_act.cu): products with the row's reciprocal scale.  `worst` returns the largest
-// distance of a product from the integer it was rounded to.  Valid for rows whose scale did not saturate
-// (|x / s_a| < 127.1, so the rounded value needs no clamp).
+// distance of a product from the integer it was rounded to.  For rows whose scale satisfies fast_scale.
 __device__ __forceinline__ uint32_t quant4_fast(uint32_t lo_pair, uint32_t hi_pair, float rinv, float& worst) {
     constexpr float MAGIC = 12582912.0f;                     // 1.5 * 2^23: adding it rounds to an integer, ties to even
     const float t0 = __fmul_rn(__uint_as_float(lo_pair << 16), rinv), t1 = __fmul_rn(__uint_as_float(lo_pair & 0xFFFF0000u), rinv);

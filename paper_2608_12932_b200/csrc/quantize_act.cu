@@ -97,8 +97,7 @@ quantize_act_kernel(const uint4* __restrict__ x, int K, uint2* __restrict__ qa,
     const __half sh = row_scale_from_amax_bits(mx);
     const float s = __half2float(sh);
     if (tid == 0) sa[m] = __half_as_ushort(sh);
-    // the fast path needs a quotient that cannot leave [-127.1, 127.1]: not for a saturated scale
-    const bool fast_row = FAST && __half_as_ushort(sh) < 0x7BFFu;
+    const bool fast_row = FAST && fast_scale(__half_as_ushort(sh));
     const float rinv = s != 0.0f ? __frcp_rn(s) : 0.0f;
 
     // chunks c..c+15 (c a multiple of 16) are one group of 128 and sit in the 16 lanes of one
@@ -184,7 +183,7 @@ silu_quantize_cluster_kernel(const uint4* __restrict__ x, int K, int C, uint2* _
     const __half sh = row_scale_from_amax_bits(mx);
     const float s = __half2float(sh);
     if (tid == 0 && rank == 0) sa[m] = __half_as_ushort(sh);
-    const bool fast_row = __half_as_ushort(sh) < 0x7BFFu;          // see quantize_act_kernel
+    const bool fast_row = fast_scale(__half_as_ushort(sh));
     const float rinv = s != 0.0f ? __frcp_rn(s) : 0.0f;
     const uint32_t seg_mask = (tid & 16) ? 0xFFFF0000u : 0x0000FFFFu;
 #pragma unroll

@@ -105,7 +105,7 @@ add_rmsnorm_quantize_kernel(const uint4* x, const uint4* r, const uint4* __restr
     const __half sh = row_scale_from_amax_bits(amax);
     const float s = __half2float(sh);
     if (tid == 0) sa[m] = __half_as_ushort(sh);
-    const bool fast_row = __half_as_ushort(sh) < 0x7BFFu;
+    const bool fast_row = fast_scale(__half_as_ushort(sh));
     const float rinv = s != 0.0f ? __frcp_rn(s) : 0.0f;
 
     // sixteen neighbouring chunks are one group of 128 and sit in the 16 lanes of one half-warp (see quantize_act_kernel)
