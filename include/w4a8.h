@@ -327,7 +327,8 @@ w4a8_status w4a8_kv8_append(const w4a8_kv8_cache* cache, const void* k_bf16, con
  * padded batch (its output is 0).  Values outside 0 .. table_width block count as the nearest.
  * Codes are multiplied as fp16, exactly; q is too (elements below 2^-31 of their row's largest are cut short); weights are
  * rounded to fp16 for the second product, sums and softmax statistics are fp32; one rounding to bf16.  Judged against the
- * fp64 definition.  A row of q with an infinity or not-a-number gives not-a-number in that row alone.
+ * fp64 definition.  A row of q with an infinity or not-a-number gives not-a-number in that row alone, and 0 where the row sees no key (limit 0,
+ * or only blocks that do not exist).  scale |q . k| of 2^126 and more, past fp32's range in base 2: that row's results are undefined.
  *   q         device, bf16, 16-byte aligned: row b T + t holds q_heads x dim contiguous values, rows q_stride elements apart
  *             (a multiple of 8, at least q_heads dim)
  *   limits    device, int32 [B][T];  out  device, bf16 [B T][q_heads dim], 16-byte aligned, not overlapping q

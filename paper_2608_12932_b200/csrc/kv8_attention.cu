@@ -192,7 +192,8 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
         run = max(run, __shfl_xor_sync(0xFFFFFFFFu, run, 2));
         const int e = kv8_row_exp(run);
         const float up = kv8_pow2(e);
-        if (t == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(smem + C::FACTOR_OFF + (rb * 16 + h * 8 + g) * 4), "f"(a.scale_log2 * kv8_pow2(-e)) : "memory");
+        const float factor = run >= 0x7F80u ? NAN : a.scale_log2 * kv8_pow2(-e);             // an infinity in the row: every score of it is not a number
+        if (t == 0) asm volatile("st.shared.f32 [%0], %1;" ::"r"(smem + C::FACTOR_OFF + (rb * 16 + h * 8 + g) * 4), "f"(factor) : "memory");
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
             // words h and 2 + h of the lane's four

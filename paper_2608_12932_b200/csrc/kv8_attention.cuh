@@ -14,6 +14,8 @@
 //     the values before they are rounded to fp16).  m is a reference, not the maximum: it moves only when a weight
 //     would pass 2^15 (256 times the reference), so sums are rescaled a few times per row, not per tile.
 //     fp16 keeps 11 bits of weights down to 2^-21 of the reference, bf16 would keep 8 of all.
+// A row of q with an infinity or not-a-number is one that both kernels mark where they form its power of two: its products alone may all be minus
+// infinity, which is what masked positions have.
 // A block of scale 0 holds zeros; 2^-80 stands for its scale (weights end at 2^-126, 2^-46 in the sum of the p, which is 2^7 / 65504 at least; and
 // weights beside it are lost only below 2^-100 of its own).
 #pragma once

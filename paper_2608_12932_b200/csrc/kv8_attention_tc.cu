@@ -41,7 +41,8 @@ struct TcCfg {
     static constexpr int KF = 0, KE = 2, VF = 4, VE = 6, SF = 8, PF = 10, QF = 14, OF = 16, MF = 18, RF = MF + TC_META, RE = RF + SLOTS, FINAL = RE + SLOTS, NUM_BARS = FINAL + 1;
     static constexpr int META_OFF = (BAR_OFF + NUM_BARS * 8 + 15) & ~15;        // [TC_META][8] float4: key scale, log2 of the value scale, its reciprocal
     static constexpr int MISC_OFF = META_OFF + TC_META * 8 * 16;                // tensor-memory base, abort flag, longest limit
-    static constexpr int SMEM = MISC_OFF + 16 + 1024;
+    static constexpr int POISON_OFF = MISC_OFF + 16;                            // per warp of 32 rows, a bit for each that is not a number
+    static constexpr int SMEM = POISON_OFF + 32 + 1024;
     static constexpr uint32_t S_COL = 0, O_COL = 256;                            // tensor memory: scores 2 x 128 columns, sums 2 x 128
 };
 
@@ -114,7 +115,11 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
             constexpr int PIECES = D / 8, PER = 32 / PIECES;  // 16-byte pieces of a row; rows per load
             const int piece = lane % PIECES, r0 = (warp & 3) * 32;
             float factor = 0.0f;
+            // A row with an infinity or not-a-number is walked as zeros and made not a number at the end, if it saw a key.  Shared memory keeps which rows
+            // these are (a register kept for it beside the walk: the prompt takes 150 instead of 147.5 us).
+            uint32_t* poisoned_at = reinterpret_cast<uint32_t*>(smem + C::POISON_OFF) + warp;
             {
+                uint32_t mine = 0;                            // largest magnitude (bf16 bits) of this thread's row
                 uint4 w[PIECES];
 #pragma unroll
                 for (int i = 0; i < PIECES; ++i) {
@@ -129,14 +134,24 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
 #pragma unroll
                     for (int o = PIECES / 2; o; o >>= 1) run = max(run, __shfl_xor_sync(0xFFFFFFFFu, run, o));
                     const int e = kv8_row_exp(run);
-                    const float up = kv8_pow2(e), down = __shfl_sync(0xFFFFFFFFu, kv8_pow2(-e), (lane % PER) * PIECES);
-                    if (lane / PER == i) factor = a.scale_log2 * down;
+                    const float up = kv8_pow2(e);
+                    const uint32_t top = __shfl_sync(0xFFFFFFFFu, run, (lane % PER) * PIECES);
+                    if (lane / PER == i) mine = top;
                     const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
                     uint32_t y[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) y[k] = kv8_pack_half2(__uint_as_float(x[k] << 16) * up, __uint_as_float(x[k] & 0xFFFF0000u) * up);
                     const int r = r0 + PER * i + lane / PIECES;
                     ptx::sts128u(base + C::Q_OFF + h * C::TILE + (piece >> 3) * C::PANEL + r * 128 + (((piece & 7) ^ (r & 7)) << 4), y[0], y[1], y[2], y[3]);
+                }
+                factor = a.scale_log2 * kv8_pow2(-kv8_row_exp(mine));
+                const bool poisoned = mine >= 0x7F80u;
+                const uint32_t which = __ballot_sync(0xFFFFFFFFu, poisoned);
+                if (lane == 0) *poisoned_at = which;
+                __syncwarp();
+                if (poisoned) {
+#pragma unroll 1
+                    for (int i = 0; i < PIECES; ++i) ptx::sts128u(base + C::Q_OFF + h * C::TILE + (i >> 3) * C::PANEL + (r0 + lane) * 128 + ((i & 7) << 4), 0u, 0u, 0u, 0u);
                 }
                 ptx::fence_proxy_async_smem();
                 __syncwarp();
@@ -245,6 +260,7 @@ kv8_attend_tiles_kernel(const __grid_constant__ AttendArgs a) {
             if (ok && n > 0) ok = ptx::warp_mbar_wait_suspend(bar(C::OF + h), 0, abort_flag);
             if (ok) {
                 ptx::tc_fence_after_sync();
+                if ((*poisoned_at >> lane & 1u) && sum != 0.0f) sum = NAN;
                 const float inv = sum == 0.0f ? 0.0f : __fdividef(1.0f, sum);
                 const size_t part = (((size_t)unit * a.tiles + tile) * a.slices + slice) * TC_ROWS + (size_t)(row - row0);
                 const uint32_t own = base + C::Q_OFF + h * C::TILE + r0 * 128;
