@@ -466,7 +466,8 @@ w4a8_status w4a8_selftest_wait_timeout(const int8_t* qa, const uint16_t* sa, con
 /*
  * Reads back the workspace status word: synchronises `stream`, returns W4A8_OK,
  * W4A8_ERR_TIMEOUT (a kernel gave up on a bounded wait; its output is then invalid) or W4A8_ERR_INDEX
- * (a kernel of the 8-bit cache met a block number or position that does not exist), and clears the word.  Host-synchronising: for tests and debugging, not for the hot path.
+ * (a kernel of the 8-bit cache met a block number or position that does not exist), and clears the word.  Where calls
+ * since the last check left both, it is W4A8_ERR_TIMEOUT.  Host-synchronising: for tests and debugging, not for the hot path.
  */
 w4a8_status w4a8_check_status(void* workspace, void* stream);
 

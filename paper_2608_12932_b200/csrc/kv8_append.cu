@@ -56,7 +56,7 @@ kv8_append_kernel(const AppendArgs a) {
     int count = a.T;
     if (a.count) count = min(max(__ldcg(a.count + seq), 0), a.T);
     if (start < 0) {
-        if (count > 0 && tid == 0) *a.status = W4A8_ERR_INDEX;
+        if (count > 0 && tid == 0) flag_index(a.status);
         return;
     }
     const long long end = (long long)start + count;
@@ -79,7 +79,7 @@ kv8_append_kernel(const AppendArgs a) {
     }
     // (the new values are on their way while the table is read, and the old scale)
     if ((unsigned)number >= (unsigned)a.num_blocks) {
-        if (tid == 0) *a.status = W4A8_ERR_INDEX;
+        if (tid == 0) flag_index(a.status);
         return;
     }
     const size_t at = (size_t)number * a.heads + head;

@@ -150,7 +150,7 @@ kv8_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
                 m.ks = __ldcg(a.k_scales + at);
                 m.vs = __ldcg(a.v_scales + at);
             } else {
-                *a.status = W4A8_ERR_INDEX;                  // positions of a block that does not exist count as not there
+                flag_index(a.status);                        // positions of a block that does not exist count as not there
             }
         }
         return m;

@@ -45,6 +45,8 @@ constexpr int BLOB_BYTES = BLOB_ZERO_OFF + TILE_N / 2;        // 8512
 //                             (all zero between calls: the tag is what says that a word has been written)
 //   [SHARED, ...)             split-K fp32 slices  [S][M][N], or the tensor-core kernel's hand-over tiles
 constexpr int WS_STATUS_OFF = 0;
+// A position that was left out is said only where nothing worse is: W4A8_ERR_TIMEOUT, an output that is invalid, replaces anything.
+__device__ __forceinline__ void flag_index(uint32_t* status) { atomicCAS(status, 0u, (uint32_t)W4A8_ERR_INDEX); }
 constexpr int WS_FUSE_SYNC_OFF = 64;
 // Each maximum carries the number of its call above 16 bits of magnitude, so a call's first maximum supersedes whatever an earlier
 // call left: nothing has to be cleared, and no kernel has to learn that every reader is done.  The projection takes the number
