@@ -265,7 +265,7 @@ w4a8_status w4a8_streaming_mask(int views, int frames, int tokens_per_frame, uin
  *   residual  the same shape, or NULL
  *   weight    device, bf16 [K], 16-byte aligned;  eps >= 0 (with 0, a row of zeros has no norm: its results are undefined)
  *   sum       receives s; required with a residual and may be the same buffer as x or as the residual (a thread reads what
- *             it then overwrites); NULL without a residual
+ *             it then overwrites); NULL without a residual, where the stream is x (W4A8_ERR_NULL where only one of the two is given)
  *   h         receives h; may be NULL; not one of the other buffers
  *   qa, sa, asum   as for w4a8_quantize_act
  * Not-a-number and infinity in a row, and a sum of squares past the fp32 range: that row's results are undefined, as for

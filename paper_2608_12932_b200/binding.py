@@ -328,7 +328,7 @@ def _bad(t, dtype, index, name):
 def w4a8_add_rmsnorm_quantize(x, weight, eps, residual=None, group=GROUP, sum_out=None, h_out=None, out=None, stream=None):
     """x, residual bf16 [M,K], weight bf16 [K] -> (s, qa int8 [M,K], sa fp16 [M], asum int32 [M,K/group]): s = x + residual in
     bf16 (x itself without a residual), the rest w4a8_quantize_act of its root-mean-square norm times weight.
-    sum_out may be x or residual; h_out receives the normed row in bf16; out = (qa, sa, asum)."""
+    sum_out, only with a residual, may be x or residual; h_out receives the normed row in bf16; out = (qa, sa, asum)."""
     index, bf16 = torch._C._cuda_getDevice(), torch.bfloat16
     if not (x.dtype is bf16 and x.get_device() == index and x.is_contiguous()):
         _bad(x, bf16, index, "x")
@@ -339,6 +339,8 @@ def w4a8_add_rmsnorm_quantize(x, weight, eps, residual=None, group=GROUP, sum_ou
     if weight.shape != (K,):
         raise W4A8Error(ERR_SHAPE, "w4a8_add_rmsnorm_quantize")
     total, r_ptr, s_ptr, h_ptr = x, None, None, None
+    if residual is None and sum_out is not None:                  # nothing would be written there
+        raise W4A8Error(ERR_NULL, "w4a8_add_rmsnorm_quantize: sum_out without a residual")
     if residual is not None:
         total = torch.empty_like(x) if sum_out is None else sum_out
         for t, name in ((residual, "residual"), (total, "sum_out")):

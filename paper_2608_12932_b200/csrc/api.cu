@@ -309,7 +309,7 @@ w4a8_status w4a8_add_rmsnorm_quantize(const void* x_bf16, const void* residual_b
                                       int group, void* sum_bf16, void* h_bf16, int8_t* qa, uint16_t* sa, int32_t* asum, void* stream) {
     if (group != GROUP || K <= 0 || K % GROUP != 0 || M < 0 || !(eps >= 0.0f)) return W4A8_ERR_SHAPE;
     if (M == 0) return W4A8_OK;
-    if (!x_bf16 || !weight_bf16 || !qa || !sa || !asum || (residual_bf16 && !sum_bf16)) return W4A8_ERR_NULL;
+    if (!x_bf16 || !weight_bf16 || !qa || !sa || !asum || !residual_bf16 != !sum_bf16) return W4A8_ERR_NULL;
     if (!aligned(x_bf16, 16) || !aligned(residual_bf16, 16) || !aligned(weight_bf16, 16) || !aligned(sum_bf16, 16) || !aligned(h_bf16, 16) ||
         !aligned(qa, 16) || !aligned(sa, 2) || !aligned(asum, 4))
         return W4A8_ERR_ALIGN;
