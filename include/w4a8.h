@@ -337,7 +337,8 @@ w4a8_status w4a8_kv8_append(const w4a8_kv8_cache* cache, const void* k_bf16, con
  * Up to 32 rows (tokens x query heads of a group) the cache streams through the kernel for few rows, above through the tcgen05
  * kernel; where row tiles are fewer than the SMs hold, the keys are split as well and a second kernel joins the sums.
  * Results are run-to-run deterministic.  W4A8_ERR_SHAPE also for q_heads not a multiple of heads, more than 65535 / heads
- * sequences, B x T >= 2^31, T q_heads / heads > 2^31 - 512, or 2^30 tiles of 256 rows and more.
+ * sequences, B x T >= 2^31, T q_heads / heads > 2^31 - 512, 2^30 tiles of 256 rows and more, or a scale that
+ * is infinite or not a number, also once multiplied by log2 e.
  */
 size_t w4a8_kv8_workspace_bytes(int dim);
 w4a8_status w4a8_kv8_attention(const w4a8_kv8_cache* cache, const void* q_bf16, long long q_stride, int B, int T, int q_heads,

@@ -1,6 +1,7 @@
 // extern "C" boundary of libw4a8: argument validation, dispatch by M, status codes.
 // Every step of the path runs in the CUDA kernels; nothing here touches the data.
 #include <cuda_runtime.h>
+#include <cmath>
 #include "host_range.h"
 #include "w4a8_internal.cuh"
 
@@ -366,7 +367,8 @@ w4a8_status w4a8_kv8_attention(const w4a8_kv8_cache* cache, const void* q_bf16, 
     if (s != W4A8_OK) return s;
     if (q_heads <= 0 || q_heads % cache->heads != 0 || q_stride % 8 != 0 || q_stride < (long long)q_heads * cache->dim ||
         (long long)T * (q_heads / cache->heads) > 0x7FFFFE00ll ||                     // row tiles are indexed with 31 bits,
-        ((long long)T * (q_heads / cache->heads) / 256 + 1) * B * cache->heads > 0x3FFFFFFFll)      // and so are the CTAs that take them
+        ((long long)T * (q_heads / cache->heads) / 256 + 1) * B * cache->heads > 0x3FFFFFFFll ||    // and so are the CTAs that take them
+        !std::isfinite(scale * KV8_LOG2_E))
         return W4A8_ERR_SHAPE;
     if (B == 0 || T == 0) return W4A8_OK;
     if (!q_bf16 || !table || !limits || !out_bf16 || !workspace) return W4A8_ERR_NULL;

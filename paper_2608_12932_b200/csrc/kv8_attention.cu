@@ -664,7 +664,7 @@ cudaError_t launch_kv8_attention(const w4a8_kv8_cache& c, const void* q, long lo
     a.log2_block = kv8_log2(c.block);
     a.tiles = p.tiles;
     a.slices = p.slices;
-    a.scale_log2 = scale * 1.44269504088896340736f;
+    a.scale_log2 = scale * KV8_LOG2_E;
     const size_t units = (size_t)B * c.heads * p.tiles * p.slices;
     a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + WS_SHARED_OFF);
     a.part_ml = reinterpret_cast<float2*>(a.part_o + units * p.rows * c.dim);

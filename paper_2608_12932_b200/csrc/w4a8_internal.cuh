@@ -118,6 +118,7 @@ cudaError_t launch_streaming_mask(int V, int F, int n, uint8_t* mask, cudaStream
 cudaError_t launch_add_rmsnorm_quantize(const void* x, const void* residual, const void* weight, float eps, int M, int K, void* sum_out,
                                         void* h_out, int8_t* qa, uint16_t* sa, int32_t* asum, cudaStream_t stream);
 // 8-bit key/value cache (w4a8_kv8_cache in the public header): append, attention.  Strides in elements; arguments checked by the caller.
+constexpr float KV8_LOG2_E = 1.44269504088896340736f;        // scores are worked in base 2
 inline int kv8_log2(int block) { return block == 16 ? 4 : (block == 32 ? 5 : (block == 64 ? 6 : 7)); }
 cudaError_t launch_kv8_append(const w4a8_kv8_cache& c, const void* k, const void* v, long long k_stride, long long v_stride, int B, int T,
                               const int32_t* table, int table_width, const int32_t* start, const int32_t* count, uint32_t* status,

@@ -35,3 +35,15 @@ def test_the_binding_does_not_either():
     assert B.w4a8_add_rmsnorm_quantize(x, w, 1e-6, residual=x, sum_out=stream)[0] is stream
     torch.cuda.synchronize()
     assert (stream == 2).all()
+
+
+@pytest.mark.parametrize("scale", [float("inf"), float("-inf"), float("nan"), 3.0e38, -3.0e38])
+def test_attention_does_not_take_a_scale_that_makes_scores_infinite(scale):
+    """In base 2 it is infinite or not a number: rows with nothing but negative products came back as zeros."""
+    f = B.lib().w4a8_kv8_attention
+    need = B.w4a8_kv8_workspace_bytes(64)
+
+    def code(scale, T=5):
+        return f(cache(), vp(0x10000), 384, 3, T, 6, vp(0x30000), 4, vp(0x40000), scale, vp(0x20000), vp(0x50000), need, None)
+    assert code(scale) == B.ERR_SHAPE and code(scale, T=0) == B.ERR_SHAPE
+    assert code(0.0, T=0) == B.OK and code(-1.0e38, T=0) == B.OK
