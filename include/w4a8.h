@@ -268,8 +268,8 @@ w4a8_status w4a8_streaming_mask(int views, int frames, int tokens_per_frame, uin
  *             it then overwrites); NULL without a residual, where the stream is x (W4A8_ERR_NULL where only one of the two is given)
  *   h         receives h; may be NULL; not one of the other buffers
  *   qa, sa, asum   as for w4a8_quantize_act
- * Not-a-number and infinity in a row, and a sum of squares past the fp32 range: that row's results are undefined, as for
- * w4a8_quantize_act.
+ * Not-a-number and infinity in a row, and a sum of squares past the fp32 range (with an eps below 2^-100 also one below that): that
+ * row's results are undefined, as for w4a8_quantize_act.
  */
 w4a8_status w4a8_add_rmsnorm_quantize(const void* x_bf16, const void* residual_bf16, const void* weight_bf16, float eps,
                                       int M, int K, int group, void* sum_bf16, void* h_bf16,
@@ -312,7 +312,7 @@ typedef struct {
  *   workspace at least W4A8_WORKSPACE_HEADER_BYTES, initialised (w4a8_workspace_init): its status word
  * The blocks that one call writes must be distinct, and not written by another call at the same time.
  * Run again on the same input it changes nothing.  Not-a-number or infinity among the new values: codes and scale of that block
- * and head are undefined, as for w4a8_quantize_act.  B, 2 heads <= 65535.
+ * and head are undefined, as for w4a8_quantize_act.  W4A8_ERR_SHAPE also for more than 65535 / heads sequences, B x T >= 2^31 and more than 32767 heads.
  */
 w4a8_status w4a8_kv8_append(const w4a8_kv8_cache* cache, const void* k_bf16, const void* v_bf16, long long k_stride,
                             long long v_stride, int B, int T, const int32_t* table, int table_width, const int32_t* start,

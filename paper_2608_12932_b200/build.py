@@ -46,7 +46,8 @@ def check_ptxas(report):
             limit = 0                             # whose roles have few registers each: a spill sits in a loop
         if spill > limit and "gemm_" in name:
             problems.append(f"{name}: {spill} bytes of spill stores")
-        if spill > 64 and ("kv8_attend" in name or "rmsnorm" in name or "kv8_append" in name or "kv8_combine" in name):
+        # (attention for many rows: the four registers that give way where a row's reference moves, which is a few times per row)
+        if spill > (16 if "kv8_attend_tiles" in name else 0) and ("kv8_attend" in name or "rmsnorm" in name or "kv8_append" in name or "kv8_combine" in name):
             problems.append(f"{name}: {spill} bytes of spill stores")
         if "gemm_tcgen05" in name or "gemm_tcshort" in name or "kv8_attend_tiles" in name:      # 512 and 640 threads share the 64 K registers
             want = 96 if "gemm_tcshort" in name else 128

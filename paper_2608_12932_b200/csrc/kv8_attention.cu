@@ -619,9 +619,13 @@ cudaError_t launch_combine(const AttendArgs& a, int B, int tile_rows, cudaStream
 
 // Row tiles of 16 with four CTAs per SM, of 32 with three, of 256 with one: what is resident at once.
 // Measured (8 key heads of 128, 1000, 4096 and 32749 positions): 16 rows 6.3, 9.7, 25.2 us as tiles of 16; 7.6, 11.3, 26.6 as tiles of 32; 10.8, 13.5, 40.1
-// as tiles of 256.  32 rows 8.2, 12.1, 27.6 as tiles of 32; 10.9, 13.4, 40.3 as tiles of 256, which take no longer for 64 rows (10.7, 13.5, 40.5).
+// as tiles of 256; all for one sequence.  32 rows 8.2, 12.1, 27.6 as tiles of 32; 10.9, 13.4, 40.3 as tiles of 256, which take no longer for 64 rows (10.7, 13.5, 40.5).
 static int ctas_per_sm(int rows) { return rows == 16 ? ArCfg<128, 1>::CTAS : (rows == 32 ? ArCfg<128, 2>::CTAS : 1); }
 
+// Slices are a whole number per row tile, so CTAs leave places empty just above a divisor of them and run a second wave just above all of them: 8 key heads,
+// 2000 positions each, draft blocks of 8 for 27, 28, 55 and 56 sequences 40, 59, 61 and 84 us; single tokens for 37, 38, 74 and 75 33, 53, 55 and 71; 16 tokens for 18
+// and 19 sequences 38 and 70.  The number goes by the table's width, not by the limits, which are on the device: one token over 4096 positions 8.5 us with
+// a table as wide, 8.9 with one 16 times as wide.
 Kv8Plan kv8_plan(int B, int T, int q_heads, int kv_heads, long long max_keys, int sms) {
     Kv8Plan p;
     const long long rows = (long long)T * (q_heads / kv_heads);

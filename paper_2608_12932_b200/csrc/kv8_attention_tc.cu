@@ -14,8 +14,8 @@
 //
 // A step's products cost 2 x 128 x 128 x D x 2 multiply-adds (2048 cycles of the tensor pipe at D = 128), its 32768 exponentials as much of the
 // special-function units, its operands and the conversion as much of shared memory's bandwidth: none of the three bounds it alone, and it takes 3000.
-// A CTA's first and last product are 5 us apart from its beginning and end.  Causal prompt of 4096, 32 heads of 128 over 8 key heads: 147 us, 935 TFLOP/s
-// at the 1.55 GHz that the power limit leaves; 200 tokens x 28 heads over 2900 positions 24.3 us; 4 views of 256 tokens over 4096 positions 70.5 us (as long as
+// A CTA's first and last product are 5 us apart from its beginning and end.  Causal prompt of 4096, 32 heads of 128 over 8 key heads: 147 us, 935 TFLOP/s,
+// in a graph of calls (156 us as a call by itself), at the 1.55 GHz that the power limit leaves; 200 tokens x 28 heads over 2900 positions 24.3 us; 4 views of 256 tokens over 4096 positions 70.5 us (as long as
 // its longest tiles, on 128 of the SMs).
 #include "kv8_attention.cuh"
 #include "quant_common.cuh"

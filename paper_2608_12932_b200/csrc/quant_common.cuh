@@ -48,6 +48,7 @@ __device__ __forceinline__ uint2 quant8(const uint4& v, float s, int& sum) {
 // within 2^-16 of their quotients).  From 2^-14 on s is amax / 127 but for a factor of 1 +- 2^-11: |x / s| < 127.1.  Below, s = n 2^-24 with amax / 127 at most
 // (n + 1/2) 2^-24: |x / s| <= 127 + 63.5 / n, which is 127.4961 for n = 128 and more from there down to 190.5 for n = 1.  At the other end a scale
 // that saturated at 65504 bounds nothing.  A scale taken from older values as well (the append's) is larger, its quotients smaller.
+// (With the division 4096 rows of 5120 take the norm 31.1 instead of 25.7 us, one row of 4096 2.5 instead of 2.3.)
 constexpr uint32_t FAST_SCALE_FIRST = 0x0080u, FAST_SCALE_END = 0x7BFFu;
 __device__ __forceinline__ bool fast_scale(uint32_t fp16_bits) {
     return fp16_bits >= FAST_SCALE_FIRST && fp16_bits < FAST_SCALE_END;
